@@ -354,6 +354,166 @@ int fademem_spectral_horizons(const double* corr, int32_t bands, int64_t lags, i
                               int64_t* horizon);
 int fademem_spectral_fit(const double* t, const double* r, int64_t n, int32_t iters, double* a, double* b);
 
+/* Rotary positions with several axes (time, height, width): the rotation a
+ * caller applies to a chunk's queries and keys.  With fademem_config's
+ * rope_pairs the memory turns its own keys by their entry index (Sec. 3.3
+ * "Boundary and positional handling"); the time axis here is the same
+ * rotation (same pairs, same frequencies, same bits).
+ * Pair p of a head turns by the angle pos[row][axis of p] * freq[p]:
+ * (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos), evaluated in fp64 and
+ * rounded once to the storage type.  The first pairs[0] pairs follow axis 0
+ * (time), the next pairs[1] axis 1 (height), the next pairs[2] axis 2 (width);
+ * pairs behind them are copied.  layout: pair p is elements (2p, 2p+1)
+ * (INTERLEAVED) or (p, p + head_dim/2) (HALVES). */
+enum { FADEMEM_ROPE_INTERLEAVED = 0, FADEMEM_ROPE_HALVES = 1 };
+enum { FADEMEM_ROPE_MAX_PAIRS = 128 };
+
+typedef struct fademem_rope {
+  int32_t head_dim;        /* multiple of 16, 16..256                          */
+  int32_t layout;          /* FADEMEM_ROPE_*                                   */
+  int32_t pairs[3];        /* >= 0 each, their sum 1..head_dim/2               */
+  double freq[FADEMEM_ROPE_MAX_PAIRS]; /* radians per position, finite         */
+} fademem_rope;
+
+/* Fill `rope` (host memory): pair k of an axis with P pairs gets the
+ * frequency theta^(-k/P).  A caller may change freq[] afterwards.
+ * Errors: EINVAL (NULL, sizes out of range, theta not in (1, 1e300)). */
+int fademem_rope_init(fademem_rope* rope, int32_t head_dim, int32_t layout, int32_t pairs_t, int32_t pairs_h,
+                      int32_t pairs_w, double theta);
+
+/* Rotate `rows` rows of `heads` heads: y[i][h] = x[i][h] turned to position
+ * pos[i] (device int32 [rows][3]; any int32 values).  x and y: device, rows
+ * x_stride / y_stride elements apart (>= heads * head_dim, a multiple of 16
+ * bytes), heads and elements contiguous, dtype FADEMEM_F32 or FADEMEM_BF16.
+ * y may be x (same stride); otherwise no row of y may overlap a row of x.
+ * inverse = 1 turns by the negative angles: the gradient with respect to x is
+ * the inverse rotation of the gradient with respect to y.  rows = 0 is a
+ * no-op.  Asynchronous on `stream`, on the current device.
+ * Errors: EINVAL (NULL/misaligned pointers, sizes, strides or overlap, a bad
+ * rotation), EHIP. */
+int fademem_rope_apply(const fademem_rope* rope, int32_t dtype, const int32_t* pos, int64_t rows, int32_t heads,
+                       const void* x, int64_t x_stride, void* y, int64_t y_stride, int32_t inverse, void* stream);
+
+/* Paged window memory: the comparison memory of Sec. 4 (the first frames as
+ * sinks that stay visible, and a sliding window of the latest ones) for many
+ * sequences at once.  K and V lie in pages of page_tokens tokens that all
+ * sequences share; a table per sequence maps its tokens to pages.  A step
+ * appends new tokens to every sequence:
+ *   fademem_paged_plan    pages, slots and positions of the step, on the GPU;
+ *   fademem_paged_insert  per layer: the step's K (rotated or not) and V into
+ *                         the pages;
+ *   fademem_paged_attend  per layer: attention of the step's queries.
+ * All three take their lengths from device memory, so a captured graph of
+ * them replays with other lengths; none waits for the device.
+ *
+ * Visibility.  Token p of a sequence lies in block b = p / block_tokens.  Its
+ * query sees the sequence's held tokens of blocks <= b that are among the
+ * first `sinks` blocks or the last `window` blocks up to b (window = 0: all
+ * of them).  block_tokens = 1 is the causal mask of a language model;
+ * block_tokens = a chunk's tokens lets the tokens of a chunk see each other
+ * and a window of chunks.
+ *
+ * Rows.  A step's rows (of q, k, v, out) are the new tokens of sequence 0,
+ * then of sequence 1, ...; row i of sequence s is row q_start[s] + i.  Rows
+ * behind the last sequence's are neither read nor written.
+ *
+ * The pool, the calls' buffers and the stream are used as fademem_cache uses
+ * its own: one store is used by one host thread and one stream at a time (its
+ * plan and its scratch too: two captured graphs of one store must not replay
+ * at the same time).  Calls are made with the device current that was
+ * current at creation (EINVAL otherwise).  FADEMEM_SERIALIZE works as above. */
+typedef struct fademem_paged_config {
+  int32_t seqs;          /* sequences, 1..1024                                  */
+  int32_t layers;        /* 1..4096; all layers share tables and page numbers  */
+  int32_t heads;         /* query heads, a multiple of kv_heads                */
+  int32_t kv_heads;      /* >= 1                                               */
+  int32_t head_dim;      /* 64 or 128                                          */
+  int32_t dtype;         /* FADEMEM_F32 or FADEMEM_BF16 for K, V, Q, O         */
+  int32_t page_tokens;   /* P, 1..65536.  Multiples of 64 are read fastest     */
+  int32_t sinks;         /* S >= 0, first blocks that stay visible             */
+  int64_t pages;         /* pages of the pool, 1..2^24                         */
+  int64_t max_tokens;    /* tokens of one sequence at most, 1..2^30            */
+  int64_t max_rows;      /* rows of one step at most, 1..2^24                  */
+  int64_t block_tokens;  /* B, 1..2^30                                         */
+  int64_t window;        /* blocks; 0: everything held is visible              */
+  int32_t grid_h;        /* token p's position is (p / (grid_h * grid_w),      */
+  int32_t grid_w;        /* p / grid_w % grid_h, p % grid_w); 1 x 1: (p, 0, 0) */
+} fademem_paged_config;
+
+typedef struct fademem_paged fademem_paged; /* opaque host object */
+
+/* Bytes of device pool: tables, the step's plan, the attention's scratch for
+ * split work, and per layer [pages][K|V][kv_heads][page_tokens][head_dim].
+ * Errors: EINVAL. */
+int fademem_paged_bytes(const fademem_paged_config* cfg, size_t* bytes);
+
+/* Create a store over a caller-owned pool (256-byte aligned); every sequence
+ * empty, every page free.  Enqueues the initialisation on `stream`; the pages'
+ * contents are left as they are.  Errors: EINVAL, ENOMEM, EHIP. */
+int fademem_paged_create(const fademem_paged_config* cfg, void* dev_pool, size_t pool_bytes, void* stream,
+                         fademem_paged** out);
+int fademem_paged_destroy(fademem_paged* paged);
+
+/* Plan a step: sequence s keeps its first kept[s] tokens (fewer than it
+ * holds: it goes back, so that a chunk can be denoised again or rejected
+ * tokens dropped; 0: it starts again) and appends added[s] tokens behind them.
+ * kept, added: device int32 [seqs], read when the stream gets there.  rows:
+ * rows of the step's buffers, at least the sum of added; max_new: the most
+ * that any added[s] is (it chooses the attention kernel).
+ * Pages that lie wholly between the sinks and the window of token kept[s], or
+ * behind the new end, are given back; then the lowest free page numbers go to
+ * the sequences in order.  The same call again changes nothing.
+ * status[s]: OK; EINVAL: kept[s] < 0 or above what is held, added[s] < 0 or
+ * > max_new, more than max_tokens or `rows` in all (nothing of s changes);
+ * ESTATE: kept[s] is behind pages already given back (nothing changes);
+ * ENOMEM: not enough free pages for it and the sequences before it (it keeps
+ * its first kept[s] tokens; no later sequence gets pages either).  The rows
+ * of such a sequence are not inserted (slot -1), and their attention is 0,
+ * LSE minus infinity.
+ * Errors: EINVAL (NULL, rows outside 0..max_rows, max_new outside 0..rows),
+ * EHIP. */
+int fademem_paged_plan(fademem_paged* paged, const int32_t* kept, const int32_t* added, int64_t rows, int64_t max_new,
+                       void* stream);
+
+/* Device arrays of the store, *count elements (NULL: not wanted): valid for
+ * its lifetime, written by fademem_paged_plan (PAGES: by
+ * fademem_paged_insert).  Reads host state only.
+ * Errors: EINVAL (NULL, unknown array, layer out of range). */
+enum {
+  FADEMEM_PAGED_Q_START = 0,   /* int32 [seqs + 1]: first row of each sequence */
+  FADEMEM_PAGED_SLOTS = 1,     /* int64 [max_rows]: page * P + offset, or -1   */
+  FADEMEM_PAGED_POSITIONS = 2, /* int32 [max_rows][3], 0 where the slot is -1  */
+  FADEMEM_PAGED_STATUS = 3,    /* int32 [seqs]                                 */
+  FADEMEM_PAGED_HELD = 4,      /* int32 [seqs]: tokens held, with the new ones */
+  FADEMEM_PAGED_TABLE = 5,     /* int32 [seqs][ceil(max_tokens / P)], -1: none */
+  FADEMEM_PAGED_FREE = 6,      /* int32 [1]: free pages                        */
+  FADEMEM_PAGED_PAGES = 7      /* dtype, the layer's pages as laid out above   */
+};
+int fademem_paged_array(const fademem_paged* paged, int32_t which, int32_t layer, void** ptr, int64_t* count);
+
+/* Write the planned step's keys and values into layer `layer`'s pages, the
+ * keys turned to their rows' POSITIONS by `rope` (host, NULL: as they are;
+ * its head_dim is the store's).  k, v: [rows][kv_heads][head_dim], rows
+ * k_stride / v_stride elements apart (multiples of 16 bytes).
+ * Errors: EINVAL, ESTATE (no step planned yet), EHIP. */
+int fademem_paged_insert(fademem_paged* paged, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                         int64_t v_stride, const fademem_rope* rope, void* stream);
+
+/* Attention of the planned step's queries over layer `layer`'s pages, the
+ * step's own tokens among them (insert first): query head h of row i reads
+ * key head h / (heads / kv_heads); O = softmax(scale Q K^T) V over the keys
+ * that the row sees.  q, out: [rows][heads][head_dim], rows q_stride /
+ * out_stride elements apart; out must not overlap q.  scale = 0 selects
+ * 1/sqrt(D); negative scales are refused.  lse, if not NULL: [heads][rows]
+ * fp32.  Keys that a row does not see do not reach it, whatever their values
+ * (infinities and NaN too).
+ * Errors: EINVAL, ESTATE (no step planned yet), EHIP. */
+int fademem_paged_attend(fademem_paged* paged, int32_t layer, const void* q, int64_t q_stride, float scale, void* out,
+                         int64_t out_stride, float* lse, void* stream);
+
+/* hipError_t value of the last FADEMEM_EHIP on this store (0 if none). */
+int fademem_paged_last_hip_error(const fademem_paged* paged);
+
 /* hipError_t value of the last FADEMEM_EHIP on this cache (0 if none). */
 int fademem_last_hip_error(const fademem_cache* cache);
 

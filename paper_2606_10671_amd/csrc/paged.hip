@@ -1,0 +1,678 @@
+// Paged window memory: pool layout, the C ABI, the step's plan (block tables,
+// slot maps, positions, the attention's work list) and the insertion of keys
+// and values into pages.
+#include <math.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include <new>
+
+#include "paged_internal.h"
+#include "rotary_device.h"
+
+using namespace fademem;
+
+struct fademem_paged {
+  fademem_paged_config cfg;
+  PagedView view;
+  int device;
+  bool planned;
+  int64_t rows, max_new;  // of the planned step
+  bool serialize;
+  int last_hip_error;
+};
+
+namespace {
+
+hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+int hip_fail(fademem_paged* c, hipError_t e) {
+  c->last_hip_error = int(e);
+  return FADEMEM_EHIP;
+}
+
+// The end of an asynchronous call: its launch status; in serialize mode also its work's.
+int finish(fademem_paged* c, void* stream) {
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && c->serialize) {
+    e = hipStreamSynchronize(as_stream(stream));
+    if (e == hipSuccess) e = hipGetLastError();
+  }
+  return e == hipSuccess ? FADEMEM_OK : hip_fail(c, e);
+}
+
+// The start of one: the store's device has to be the current one.
+int enter(fademem_paged* c) {
+  int dev = -1;
+  (void)hipGetLastError();
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(c, e);
+  return dev == c->device ? FADEMEM_OK : FADEMEM_EINVAL;
+}
+
+// ---------------------------------------------------------------------------
+// Layout
+// ---------------------------------------------------------------------------
+
+constexpr uint64_t kMaxPool = uint64_t(1) << 46;
+
+// Row tiles of a step at most, whatever the kernel.
+int64_t max_tiles(const fademem_paged_config& c) {
+  return c.max_rows * (c.heads / c.kv_heads) / kPagedMinTileRows + c.seqs;
+}
+
+// Fills `v` with offsets from `pool` (NULL: sizes only); false: too large.
+bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* total) {
+  unsigned __int128 at = 0;
+  auto take = [&](unsigned __int128 bytes) {
+    const unsigned __int128 here = at;
+    at += (bytes + 255) / 256 * 256;
+    return pool + size_t(here);
+  };
+  memset(v, 0, sizeof *v);
+  const int64_t P = c.page_tokens, width = (c.max_tokens + P - 1) / P;
+  const size_t elt = c.dtype == FADEMEM_BF16 ? 2 : 4;
+  const unsigned __int128 seqs = unsigned(c.seqs);
+  const unsigned __int128 page = (unsigned __int128)2 * unsigned(c.kv_heads) * uint64_t(P) * unsigned(c.head_dim) * elt;
+  const unsigned __int128 layer = page * uint64_t(c.pages);
+  if (layer * unsigned(c.layers) > kMaxPool || seqs * uint64_t(width) * 4 > kMaxPool) return false;
+  const TileShape wide = c.dtype == FADEMEM_BF16 ? kPagedWideBf16 : kPagedWideF32;
+  v->pool = pool;
+  v->header = reinterpret_cast<PagedHeader*>(take(sizeof(PagedHeader)));
+  v->held = reinterpret_cast<int32_t*>(take(seqs * 4));
+  v->gone = reinterpret_cast<int32_t*>(take(seqs * 4));
+  v->status = reinterpret_cast<int32_t*>(take(seqs * 4));
+  v->first = reinterpret_cast<int32_t*>(take(seqs * 4));
+  v->added = reinterpret_cast<int32_t*>(take(seqs * 4));
+  v->q_start = reinterpret_cast<int32_t*>(take((seqs + 1) * 4));
+  v->bitmap = reinterpret_cast<uint32_t*>(take(uint64_t((c.pages + 31) / 32) * 4));
+  v->table = reinterpret_cast<int32_t*>(take(seqs * uint64_t(width) * 4));
+  v->slots = reinterpret_cast<int64_t*>(take(uint64_t(c.max_rows) * 8));
+  v->pos = reinterpret_cast<int32_t*>(take(uint64_t(c.max_rows) * 12));
+  v->tile0 = reinterpret_cast<int32_t*>(take((seqs + 1) * 4));
+  v->unit_end = reinterpret_cast<int64_t*>(take(uint64_t(max_tiles(c)) * 8));
+  v->starts = reinterpret_cast<WorkStart*>(take((kPagedMaxGroups + 1) * sizeof(WorkStart)));
+  v->redo = reinterpret_cast<uint8_t*>(take((unsigned __int128)uint64_t(max_tiles(c)) * unsigned(c.kv_heads) * 8));
+  v->scratch = reinterpret_cast<float*>(take(2 * kPagedMaxGroups * paged_slot_floats(wide.rows, c.head_dim) * 4));
+  v->pages = take(layer * unsigned(c.layers));
+  v->page_bytes = size_t(page);
+  v->layer_bytes = size_t(layer);
+  v->n_pages = c.pages;
+  v->max_tokens = c.max_tokens;
+  v->block = c.block_tokens;
+  v->window = c.window;
+  const int64_t most = int64_t(1) << 30;  // beyond every sequence
+  v->sink_tokens = c.window == 0 ? 0 : c.sinks > most / c.block_tokens ? most : int64_t(c.sinks) * c.block_tokens;
+  v->seqs = c.seqs;
+  v->heads = c.heads;
+  v->kv_heads = c.kv_heads;
+  v->group = c.heads / c.kv_heads;
+  v->head_dim = c.head_dim;
+  v->page_tokens = int32_t(P);
+  v->width = int32_t(width);
+  v->front = int32_t((v->sink_tokens + P - 1) / P);
+  v->grid_h = c.grid_h;
+  v->grid_w = c.grid_w;
+  if (at > kMaxPool) return false;
+  *total = size_t(at);
+  return true;
+}
+
+bool valid_config(const fademem_paged_config* c) {
+  const int64_t most = int64_t(1) << 30;
+  if (!c) return false;
+  if (c->seqs < 1 || c->seqs > kPagedMaxSeqs || c->layers < 1 || c->layers > 4096) return false;
+  if (c->kv_heads < 1 || c->heads < c->kv_heads || c->heads > 4096 || c->heads % c->kv_heads) return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->dtype != FADEMEM_F32 && c->dtype != FADEMEM_BF16) return false;
+  if (c->page_tokens < 1 || c->page_tokens > 65536 || c->pages < 1 || c->pages > (int64_t(1) << 24)) return false;
+  if (c->max_tokens < 1 || c->max_tokens > most || c->max_rows < 1 || c->max_rows > (int64_t(1) << 24)) return false;
+  if (c->max_rows * (c->heads / c->kv_heads) > most) return false;
+  if (c->block_tokens < 1 || c->block_tokens > most || c->window < 0 || c->window > most) return false;
+  if (c->sinks < 0) return false;
+  if (c->grid_h < 1 || c->grid_w < 1 || int64_t(c->grid_h) * c->grid_w > most) return false;
+  return true;
+}
+
+// ---------------------------------------------------------------------------
+// Kernels
+// ---------------------------------------------------------------------------
+
+__global__ void paged_init_kernel(PagedView v, int64_t words, int64_t entries) {
+  const int64_t step = int64_t(gridDim.x) * blockDim.x, i0 = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (i0 == 0) {
+    v.header->free = int32_t(v.n_pages);
+    v.header->groups = 0;
+    v.q_start[v.seqs] = 0;
+  }
+  for (int64_t i = i0; i < v.seqs; i += step) {
+    v.held[i] = v.status[i] = v.first[i] = v.added[i] = v.q_start[i] = 0;
+    v.gone[i] = v.front;
+  }
+  for (int64_t i = i0; i < words; i += step) {
+    const int64_t left = v.n_pages - i * 32;
+    v.bitmap[i] = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
+  }
+  for (int64_t i = i0; i < entries; i += step) v.table[i] = -1;
+}
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / 64;
+
+// Inclusive prefix sum over the block; `total` gets the sum.
+__device__ int64_t block_scan(int64_t x, int64_t* red, int64_t* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) red[wave] = x;
+  __syncthreads();
+  int64_t before = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    if (w < wave) before += red[w];
+    sum += red[w];
+  }
+  __syncthreads();
+  *total = sum;
+  return before + x;
+}
+
+// Last i in [0, n) with a[i] <= x (a[0] <= x, a not decreasing).
+template <class T>
+__device__ __forceinline__ int last_at_most(const T* a, int n, T x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+struct PlanArgs {
+  PagedView v;
+  const int32_t* kept;
+  const int32_t* added;
+  int64_t rows, max_new;
+  TileShape shape;
+  int max_groups;
+  int min_units;  // units of a workgroup at least
+};
+
+// The step's plan, one block: thread s has sequence s.  What each sequence gives
+// back and needs follows from its lengths alone; prefix sums over the sequences
+// say where its rows, pages and row tiles begin.  Pages are bits of a map, so
+// "the lowest free page" does not depend on the order in which pages came back.
+__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
+  const PagedView& v = a.v;
+  __shared__ int64_t red[kPlanWaves];
+  __shared__ int64_t pre[kPagedMaxSeqs + 1];  // prefix sums of what the phase deals out
+  __shared__ int32_t r1_lo[kPagedMaxSeqs], r1_n[kPagedMaxSeqs], r2_lo[kPagedMaxSeqs];
+  const int tid = threadIdx.x, s = tid, seqs = v.seqs;
+  const bool live = s < seqs;
+  const int64_t P = v.page_tokens;
+  int64_t total;
+
+  // Lengths, checked.
+  const int64_t k = live ? a.kept[s] : 0, n = live ? a.added[s] : 0, held = live ? v.held[s] : 0;
+  const int32_t gone = live ? v.gone[s] : 0;
+  const int64_t want_rows = live && n > 0 ? n : 0;
+  const int64_t row_end = block_scan(want_rows, red, &total);
+  const int64_t row_total = total;
+  int32_t code = FADEMEM_OK;
+  if (k < 0 || n < 0 || n > a.max_new || k > held || k + n > v.max_tokens || (n > 0 && row_end > a.rows))
+    code = FADEMEM_EINVAL;
+  const int32_t front = v.front;
+  const int64_t low_page = code ? 0 : paged_low(v, k) / P;
+  const bool restart = gone > front && k <= front * P;  // all that is kept lies in the sinks' pages
+  if (!code && gone > front && !restart && low_page < gone) code = FADEMEM_ESTATE;
+  const bool ok = live && code == FADEMEM_OK;
+
+  // Pages that go (two ranges) and pages needed, for `m` new tokens.
+  const int32_t top = int32_t(low_page > front ? low_page : front);
+  const int32_t np_old = int32_t((held + P - 1) / P);
+  int32_t lo1 = 0, n1 = 0, lo2 = 0, n2 = 0, need = 0, from = 0;
+  auto pages_for = [&](int64_t m) {
+    const int32_t np = int32_t((k + m + P - 1) / P);
+    n1 = n2 = need = 0;
+    if (!ok) return;
+    if (restart) {
+      lo1 = np;
+      n1 = max(0, min(front, np_old) - np);
+      lo2 = gone;
+      n2 = max(0, np_old - gone);
+      from = front;
+    } else {
+      lo1 = gone;
+      n1 = max(0, min(top, np_old) - gone);
+      lo2 = np;
+      n2 = max(0, np_old - np);
+      from = np_old;
+    }
+    need = max(0, np - from);
+  };
+  pages_for(n);
+  const int64_t free0 = v.header->free;
+  block_scan(n1 + n2, red, &total);
+  const int64_t avail = free0 + total;
+  const int64_t need_end = block_scan(need, red, &total);
+  if (ok && need > 0 && need_end > avail) {
+    code = FADEMEM_ENOMEM;
+    pages_for(0);
+  }
+  const bool admitted = ok && code == FADEMEM_OK;
+
+  // Release.
+  int64_t released;
+  {
+    const int64_t end = block_scan(n1 + n2, red, &released);
+    if (live) {
+      pre[s] = end - n1 - n2;
+      r1_lo[s] = lo1;
+      r1_n[s] = n1;
+      r2_lo[s] = lo2;
+    }
+    __syncthreads();
+    for (int64_t i = tid; i < released; i += kPlanThreads) {
+      const int q = last_at_most<int64_t>(pre, seqs, i);
+      const int32_t o = int32_t(i - pre[q]);
+      const int32_t idx = o < r1_n[q] ? r1_lo[q] + o : r2_lo[q] + o - r1_n[q];
+      int32_t* e = v.table + size_t(q) * v.width + idx;
+      const int32_t page = *e;
+      *e = -1;
+      if (page >= 0 && page < v.n_pages) atomicOr(v.bitmap + (page >> 5), 1u << (page & 31));
+    }
+    __syncthreads();
+  }
+
+  // Allocation: the i-th lowest free page is the i-th needed one.
+  int64_t given;
+  {
+    const int64_t end = block_scan(need, red, &given);
+    if (live) {
+      pre[s] = end - need;
+      r1_lo[s] = from;
+    }
+    __syncthreads();
+    const int64_t words = (v.n_pages + 31) / 32;
+    int64_t rank0 = 0;
+    for (int64_t w0 = 0; w0 < words && rank0 < given; w0 += kPlanThreads) {
+      const int64_t w = w0 + tid;
+      uint32_t bits = w < words ? __hip_atomic_load(v.bitmap + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+      int64_t found;
+      const int cnt = __popc(bits);
+      int64_t rank = rank0 + block_scan(cnt, red, &found) - cnt;
+      const uint32_t before = bits;
+      while (bits && rank < given) {
+        const int b = __ffs(bits) - 1;
+        bits &= bits - 1;
+        const int q = last_at_most<int64_t>(pre, seqs, rank);
+        v.table[size_t(q) * v.width + r1_lo[q] + int32_t(rank - pre[q])] = int32_t(w * 32 + b);
+        ++rank;
+      }
+      if (bits != before) __hip_atomic_store(v.bitmap + w, bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      rank0 += found;
+    }
+    __syncthreads();
+  }
+
+  // State.
+  const int64_t fresh = admitted ? n : 0;
+  if (live) {
+    v.status[s] = code;
+    v.first[s] = int32_t(ok ? k : 0);
+    v.added[s] = int32_t(fresh);
+    v.q_start[s] = int32_t(min(row_end - want_rows, a.rows));
+    if (ok) {
+      v.held[s] = int32_t(k + fresh);
+      v.gone[s] = top;
+    }
+  }
+  if (tid == 0) {
+    v.q_start[seqs] = int32_t(min(row_total, a.rows));
+    v.header->free = int32_t(free0 + released - given);
+  }
+
+  // The attention's work: row tiles, their key units, where each workgroup starts.
+  const int G = v.group;
+  const int tiles_s = int((fresh * G + a.shape.rows - 1) / a.shape.rows);
+  int64_t n_tiles;
+  const int64_t tile_end = block_scan(tiles_s, red, &n_tiles);
+  if (live) {
+    pre[s] = tile_end - tiles_s;
+    v.tile0[s] = int32_t(tile_end - tiles_s);
+    r1_lo[s] = int32_t(k);
+    r2_lo[s] = int32_t(fresh);
+  }
+  if (tid == 0) {
+    pre[seqs] = n_tiles;
+    v.tile0[seqs] = int32_t(n_tiles);
+  }
+  __syncthreads();
+  int64_t units0 = 0;
+  for (int64_t t0 = 0; t0 < n_tiles; t0 += kPlanThreads) {
+    const int64_t t = t0 + tid;
+    int64_t units = 0, sum;
+    if (t < n_tiles) {
+      const int q = last_at_most<int64_t>(pre, seqs, t);
+      const int64_t row0 = (t - pre[q]) * a.shape.rows, row1 = min(row0 + a.shape.rows, int64_t(r2_lo[q]) * G);
+      const int64_t p = r1_lo[q];
+      units = tile_span(v, p + row0 / G, p + (row1 - 1) / G, p + r2_lo[q], a.shape.unit_keys).n_units;
+    }
+    const int64_t end = units0 + block_scan(units, red, &sum);
+    if (t < n_tiles) v.unit_end[t] = end;
+    units0 += sum;
+  }
+  __syncthreads();
+  const int64_t all = units0 * v.kv_heads;
+  int groups = int(min(int64_t(a.max_groups), (all + a.min_units - 1) / a.min_units));
+  if (tid <= groups) {
+    WorkStart w = {seqs, 0, int32_t(n_tiles), 0};
+    if (tid < groups) {
+      const int64_t at = all * tid / groups;
+      // Sequence: the last one whose units begin at or before `at` and that has units.
+      int lo = 0, hi = seqs;
+      auto begin = [&](int q) { return pre[q] > 0 ? v.unit_end[pre[q] - 1] : int64_t(0); };
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (begin(mid) * v.kv_heads <= at) lo = mid;
+        else hi = mid;
+      }
+      const int64_t base = begin(lo), per_head = begin(lo + 1) - base, local = at - base * v.kv_heads;
+      w.seq = lo;
+      w.head = int32_t(local / per_head);
+      const int64_t x = base + local % per_head;  // unit of the sequence's tiles
+      int64_t t = pre[lo], e = pre[lo + 1];       // first tile whose units end behind x
+      while (t < e) {
+        const int64_t mid = (t + e) >> 1;
+        if (v.unit_end[mid] > x) e = mid;
+        else t = mid + 1;
+      }
+      w.tile = int32_t(t);
+      w.unit = int32_t(x - (t > 0 ? v.unit_end[t - 1] : 0));
+    }
+    v.starts[tid] = w;
+  }
+  if (tid == 0) v.header->groups = groups;
+}
+
+// Slot and position of every row of the step.
+constexpr int kFillThreads = 256;
+__global__ __launch_bounds__(kFillThreads) void paged_rows_kernel(PagedView v, int64_t rows) {
+  __shared__ int32_t start[kPagedMaxSeqs + 1];
+  for (int i = threadIdx.x; i <= v.seqs; i += kFillThreads) start[i] = v.q_start[i];
+  __syncthreads();
+  const int64_t i = int64_t(blockIdx.x) * kFillThreads + threadIdx.x;
+  if (i >= rows) return;
+  int64_t slot = -1;
+  int32_t t = 0, y = 0, x = 0;
+  if (i < start[v.seqs]) {
+    const int s = last_at_most<int32_t>(start, v.seqs, int32_t(i));
+    const int32_t o = int32_t(i) - start[s];
+    if (o < v.added[s]) {
+      const int32_t p = v.first[s] + o, frame = v.grid_h * v.grid_w;
+      const int32_t page = p / v.page_tokens;
+      slot = int64_t(v.table[size_t(s) * v.width + page]) * v.page_tokens + (p - page * v.page_tokens);
+      t = p / frame;
+      y = (p - t * frame) / v.grid_w;
+      x = p - t * frame - y * v.grid_w;
+    }
+  }
+  v.slots[i] = slot;
+  v.pos[3 * i] = t;
+  v.pos[3 * i + 1] = y;
+  v.pos[3 * i + 2] = x;
+}
+
+struct PagedInsertArgs {
+  const char* k;
+  const char* v;
+  size_t k_pitch, v_pitch;  // bytes between rows
+  char* pages;              // of the layer
+  size_t page_bytes;
+  int64_t n_slots;          // pages * page_tokens
+  const int64_t* slots;
+  const int32_t* pos;
+  int64_t rows;
+  int kv_heads, head_dim, page_tokens;
+  int per_block;            // rows of a block
+  RotaryArg rot;            // pairs = 0: keys as they are
+};
+
+// Rows into the pages of their slots.  As rope_kernel, with the keys' units
+// first and the values' behind them; a unit goes to
+// [page][K|V][head][offset][element].
+template <bool BF16, bool HALVES>
+__global__ __launch_bounds__(kRotThreads) void paged_insert_kernel(PagedInsertArgs a) {
+  extern __shared__ __attribute__((aligned(16))) double2 cs[];
+  constexpr int kElts = BF16 ? 8 : 4;
+  const int64_t row0 = int64_t(blockIdx.x) * a.per_block;
+  const int n = int(min(int64_t(a.per_block), a.rows - row0));
+  if (a.rot.pairs > 0) {
+    rotary_angles(a.rot, a.pos, row0, n, cs);
+    __syncthreads();
+  }
+  const int head_units = a.head_dim / kElts, half = head_units / 2;
+  const int k_head = HALVES ? half : head_units;
+  const int k_row = a.kv_heads * k_head, v_row = a.kv_heads * head_units, per_row = k_row + v_row;
+  const size_t head_pitch = size_t(a.page_tokens) * head_units;  // units between heads of a page
+  for (int i = threadIdx.x; i < n * per_row; i += kRotThreads) {
+    const int t = i / per_row;
+    int r = i - t * per_row;
+    const int64_t slot = a.slots[row0 + t];
+    if (slot < 0 || slot >= a.n_slots) continue;
+    const int64_t page = slot / a.page_tokens, off = slot - page * a.page_tokens;
+    rot_u32x4* base = reinterpret_cast<rot_u32x4*>(a.pages + size_t(page) * a.page_bytes) + off * head_units;
+    if (r < k_row) {
+      const int h = r / k_head, u = r - h * k_head;
+      const rot_u32x4* src = reinterpret_cast<const rot_u32x4*>(a.k + size_t(row0 + t) * a.k_pitch) + h * head_units + u;
+      rot_u32x4* dst = base + h * head_pitch + u;
+      const double2* c = cs + t * a.rot.pairs;
+      if constexpr (HALVES) {
+        rot_u32x4 p = src[0], q = src[half];
+        rotate_halves<BF16>(p, q, c, u * kElts, a.rot.pairs);
+        dst[0] = p;
+        dst[half] = q;
+      } else {
+        dst[0] = rotate_unit<BF16>(src[0], c, u * (kElts / 2), a.rot.pairs);
+      }
+    } else {
+      r -= k_row;
+      const int h = r / head_units, u = r - h * head_units;
+      base[(a.kv_heads + h) * head_pitch + u] =
+          reinterpret_cast<const rot_u32x4*>(a.v + size_t(row0 + t) * a.v_pitch)[h * head_units + u];
+    }
+  }
+}
+
+bool narrow_step(const fademem_paged* c) {
+  return c->max_new * c->view.group <= kPagedNarrowBf16.rows;
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// C ABI
+// ---------------------------------------------------------------------------
+
+extern "C" {
+
+int fademem_paged_bytes(const fademem_paged_config* cfg, size_t* bytes) {
+  PagedView v;
+  size_t total = 0;
+  if (!bytes || !valid_config(cfg) || !lay_out(*cfg, nullptr, &v, &total)) return FADEMEM_EINVAL;
+  *bytes = total;
+  return FADEMEM_OK;
+}
+
+int fademem_paged_create(const fademem_paged_config* cfg, void* dev_pool, size_t pool_bytes, void* stream,
+                         fademem_paged** out) {
+  if (!out) return FADEMEM_EINVAL;
+  *out = nullptr;
+  PagedView v;
+  size_t total = 0;
+  if (!valid_config(cfg) || !dev_pool || !aligned(dev_pool, 256)) return FADEMEM_EINVAL;
+  if (!lay_out(*cfg, static_cast<char*>(dev_pool), &v, &total)) return FADEMEM_EINVAL;
+  if (pool_bytes < total) return FADEMEM_ENOMEM;
+  fademem_paged* c = new (std::nothrow) fademem_paged();
+  if (!c) return FADEMEM_ENOMEM;
+  c->cfg = *cfg;
+  c->view = v;
+  c->planned = false;
+  c->rows = c->max_new = 0;
+  const char* ser = getenv("FADEMEM_SERIALIZE");
+  c->serialize = ser && ser[0] && strcmp(ser, "0") != 0;
+  c->last_hip_error = 0;
+  (void)hipGetLastError();
+  if (hipGetDevice(&c->device) != hipSuccess) {
+    delete c;
+    return FADEMEM_EHIP;
+  }
+  const int64_t words = (cfg->pages + 31) / 32, entries = int64_t(cfg->seqs) * v.width;
+  const int64_t blocks = (entries + 255) / 256;
+  hipLaunchKernelGGL(paged_init_kernel, dim3(unsigned(blocks < 1024 ? blocks : 1024)), dim3(256), 0, as_stream(stream),
+                     v, words, entries);
+  if (int rc = finish(c, stream)) {
+    delete c;
+    return rc;
+  }
+  *out = c;
+  return FADEMEM_OK;
+}
+
+int fademem_paged_destroy(fademem_paged* paged) {
+  delete paged;
+  return FADEMEM_OK;
+}
+
+int fademem_paged_last_hip_error(const fademem_paged* paged) { return paged ? paged->last_hip_error : 0; }
+
+int fademem_paged_plan(fademem_paged* c, const int32_t* kept, const int32_t* added, int64_t rows, int64_t max_new,
+                       void* stream) {
+  if (!c || !kept || !added || !aligned(kept, 4) || !aligned(added, 4)) return FADEMEM_EINVAL;
+  if (rows < 0 || rows > c->cfg.max_rows || max_new < 0 || max_new > rows) return FADEMEM_EINVAL;
+  if (int rc = enter(c)) return rc;
+  c->rows = rows;
+  c->max_new = max_new;
+  PlanArgs a;
+  a.v = c->view;
+  a.kept = kept;
+  a.added = added;
+  a.rows = rows;
+  a.max_new = max_new;
+  const bool narrow = narrow_step(c);
+  a.shape = c->cfg.dtype == FADEMEM_BF16 ? (narrow ? kPagedNarrowBf16 : kPagedWideBf16)
+                                         : (narrow ? kPagedNarrowF32 : kPagedWideF32);
+  a.max_groups = kPagedMaxGroups;
+  a.min_units = narrow ? 1 : 4;
+  hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, as_stream(stream), a);
+  if (rows > 0)
+    hipLaunchKernelGGL(paged_rows_kernel, dim3(unsigned((rows + kFillThreads - 1) / kFillThreads)), dim3(kFillThreads), 0,
+                       as_stream(stream), c->view, rows);
+  const int rc = finish(c, stream);
+  c->planned = rc == FADEMEM_OK;
+  return rc;
+}
+
+int fademem_paged_array(const fademem_paged* c, int32_t which, int32_t layer, void** ptr, int64_t* count) {
+  if (!c || !ptr) return FADEMEM_EINVAL;
+  const PagedView& v = c->view;
+  void* p = nullptr;
+  int64_t n = 0;
+  switch (which) {
+    case FADEMEM_PAGED_Q_START: p = v.q_start; n = v.seqs + 1; break;
+    case FADEMEM_PAGED_SLOTS: p = v.slots; n = c->cfg.max_rows; break;
+    case FADEMEM_PAGED_POSITIONS: p = v.pos; n = c->cfg.max_rows * 3; break;
+    case FADEMEM_PAGED_STATUS: p = v.status; n = v.seqs; break;
+    case FADEMEM_PAGED_HELD: p = v.held; n = v.seqs; break;
+    case FADEMEM_PAGED_TABLE: p = v.table; n = int64_t(v.seqs) * v.width; break;
+    case FADEMEM_PAGED_FREE: p = &v.header->free; n = 1; break;
+    case FADEMEM_PAGED_PAGES:
+      if (layer < 0 || layer >= c->cfg.layers) return FADEMEM_EINVAL;
+      p = v.pages + size_t(layer) * v.layer_bytes;
+      n = int64_t(v.layer_bytes / (c->cfg.dtype == FADEMEM_BF16 ? 2 : 4));
+      break;
+    default: return FADEMEM_EINVAL;
+  }
+  *ptr = p;
+  if (count) *count = n;
+  return FADEMEM_OK;
+}
+
+int fademem_paged_insert(fademem_paged* c, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                         int64_t v_stride, const fademem_rope* rope, void* stream) {
+  if (!c || layer < 0 || layer >= c->cfg.layers) return FADEMEM_EINVAL;
+  const int elt = c->cfg.dtype == FADEMEM_BF16 ? 2 : 4;
+  const int64_t row = int64_t(c->cfg.kv_heads) * c->cfg.head_dim;
+  PagedInsertArgs a;
+  memset(&a.rot, 0, sizeof a.rot);
+  if (rope) {
+    if (int rc = rotary_arg(rope, 0, &a.rot)) return rc;
+    if (a.rot.head_dim != c->cfg.head_dim) return FADEMEM_EINVAL;
+  }
+  for (int64_t s : {k_stride, v_stride})
+    if (s < row || s > (int64_t(1) << 32) || s * elt % 16) return FADEMEM_EINVAL;
+  if (!c->planned) return FADEMEM_ESTATE;
+  if (c->rows == 0) return FADEMEM_OK;
+  if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return FADEMEM_EINVAL;
+  if (int rc = enter(c)) return rc;
+  a.k = static_cast<const char*>(k);
+  a.v = static_cast<const char*>(v);
+  a.k_pitch = size_t(k_stride) * elt;
+  a.v_pitch = size_t(v_stride) * elt;
+  a.pages = c->view.pages + size_t(layer) * c->view.layer_bytes;
+  a.page_bytes = c->view.page_bytes;
+  a.n_slots = c->cfg.pages * c->cfg.page_tokens;
+  a.slots = c->view.slots;
+  a.pos = c->view.pos;
+  a.rows = c->rows;
+  a.kv_heads = c->cfg.kv_heads;
+  a.head_dim = c->cfg.head_dim;
+  a.page_tokens = c->cfg.page_tokens;
+  const int per_row = int(2 * row * elt / 16);
+  int64_t per = 1024 / per_row;
+  if (per > (a.rows + 511) / 512) per = (a.rows + 511) / 512;
+  a.per_block = int(per < 1 ? 1 : per > kRotMaxRows ? kRotMaxRows : per);
+  const bool bf16 = c->cfg.dtype == FADEMEM_BF16, halves = rope && a.rot.halves;
+  auto kernel = bf16 ? (halves ? paged_insert_kernel<true, true> : paged_insert_kernel<true, false>)
+                     : (halves ? paged_insert_kernel<false, true> : paged_insert_kernel<false, false>);
+  hipLaunchKernelGGL(kernel, dim3(unsigned((a.rows + a.per_block - 1) / a.per_block)), dim3(kRotThreads),
+                     size_t(a.per_block) * a.rot.pairs * sizeof(double2), as_stream(stream), a);
+  return finish(c, stream);
+}
+
+int fademem_paged_attend(fademem_paged* c, int32_t layer, const void* q, int64_t q_stride, float scale, void* out,
+                         int64_t out_stride, float* lse, void* stream) {
+  if (!c || layer < 0 || layer >= c->cfg.layers) return FADEMEM_EINVAL;
+  if (!(scale >= 0.0f) || !isfinite(scale)) return FADEMEM_EINVAL;
+  const int elt = c->cfg.dtype == FADEMEM_BF16 ? 2 : 4;
+  const int64_t row = int64_t(c->cfg.heads) * c->cfg.head_dim;
+  for (int64_t s : {q_stride, out_stride})
+    if (s < row || s > (int64_t(1) << 32) || s * elt % 16) return FADEMEM_EINVAL;
+  if (!c->planned) return FADEMEM_ESTATE;
+  if (c->rows == 0) return FADEMEM_OK;
+  if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4)) return FADEMEM_EINVAL;
+  if (!rows_apart(static_cast<const char*>(q), size_t(q_stride) * elt, static_cast<const char*>(out),
+                  size_t(out_stride) * elt, c->rows, size_t(row) * elt))
+    return FADEMEM_EINVAL;
+  if (int rc = enter(c)) return rc;
+  PagedAttendArgs a;
+  a.v = c->view;
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.pages = c->view.pages + size_t(layer) * c->view.layer_bytes;
+  a.q_pitch = size_t(q_stride) * elt;
+  a.out_pitch = size_t(out_stride) * elt;
+  a.rows = c->rows;
+  a.scale = scale == 0.0f ? 1.0f / sqrtf(float(c->cfg.head_dim)) : scale;
+  const hipError_t e = launch_paged_attend(a, c->cfg.dtype == FADEMEM_BF16, narrow_step(c), as_stream(stream));
+  if (e != hipSuccess) return hip_fail(c, e);
+  return finish(c, stream);
+}
+
+}  // extern "C"

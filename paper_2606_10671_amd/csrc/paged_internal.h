@@ -1,0 +1,129 @@
+// Paged window memory: what its translation units share (not public).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "fademem.h"
+
+namespace fademem {
+
+constexpr int kPagedMaxSeqs = 1024;   // one thread of the plan kernel per sequence
+constexpr int kPagedMaxGroups = 256;  // workgroups of one attention launch at most (one per CU)
+
+// Attention work of a step.  The rows of a tile are (token, head of the group)
+// pairs of one sequence and one key head, token-major: row r is token r / G,
+// head r % G of the key head's G query heads, so that a tile of K and V serves
+// all of them.  A tile's keys come in units of `unit_keys`: first the units
+// that cover the sinks, then those that cover the window.  All units of a step
+// lie on one line, ordered by (sequence, key head, tile, unit), and are dealt
+// to the workgroups in equal runs: a run may end one tile's units, take some
+// tiles whole and begin another's.  Units of a tile that several workgroups
+// share leave partial results in their slots (0: a run's first units, which
+// continue a tile; 1: its last units, which begin one).
+struct WorkStart {
+  int32_t seq, head, tile, unit;  // tile: over all sequences; unit: within the tile
+};
+
+// Tile and key-unit shapes of an attention kernel.
+struct TileShape {
+  int rows;       // query rows of a tile
+  int unit_keys;  // keys of a unit
+};
+constexpr TileShape kPagedWideBf16 = {256, 64};
+constexpr TileShape kPagedNarrowBf16 = {32, 256};
+constexpr TileShape kPagedWideF32 = {128, 64};
+constexpr TileShape kPagedNarrowF32 = {32, 128};
+constexpr int kPagedMinTileRows = 32;
+
+// Floats of a partial result of a tile: O of every row, then row max and row sum.
+__host__ __device__ constexpr size_t paged_slot_floats(int rows, int head_dim) {
+  return size_t(rows) * size_t(head_dim + 2);
+}
+
+struct PagedHeader {
+  int32_t free;    // free pages
+  int32_t groups;  // workgroups with work (attention)
+};
+
+// The store as kernels see it.
+struct PagedView {
+  char* pool;
+  PagedHeader* header;
+  int32_t* held;       // [seqs] tokens held
+  int32_t* gone;       // [seqs] first page behind the sinks' that is still mapped
+  int32_t* status;     // [seqs]
+  int32_t* first;      // [seqs] position of the step's first new token
+  int32_t* added;      // [seqs] new tokens of the step that were admitted
+  int32_t* q_start;    // [seqs + 1]
+  uint32_t* bitmap;    // [words] bit = 1: the page is free
+  int32_t* table;      // [seqs][width]
+  int64_t* slots;      // [max_rows]
+  int32_t* pos;        // [max_rows][3]
+  int32_t* tile0;      // [seqs + 1] first row tile of each sequence
+  int64_t* unit_end;   // [tiles] units of one head up to and with each tile
+  WorkStart* starts;   // [groups + 1]
+  uint8_t* redo;       // [tiles][kv_heads][8]: the rows of a tile's wave have to be worked out again
+  float* scratch;      // attention partials
+  char* pages;         // layer 0
+  size_t layer_bytes;
+  size_t page_bytes;
+  int64_t n_pages;
+  int64_t max_tokens;
+  int64_t block;       // B
+  int64_t window;      // W, 0: everything
+  int64_t sink_tokens; // S * B (0 without a window)
+  int32_t seqs, heads, kv_heads, group, head_dim;
+  int32_t page_tokens, width;
+  int32_t front;       // pages that hold sinks
+  int32_t grid_h, grid_w;
+};
+
+// First key of the window of a query at position p, and the end of what it sees.
+__host__ __device__ inline int64_t paged_low(const PagedView& v, int64_t p) {
+  if (v.window == 0) return 0;
+  const int64_t b = p / v.block - v.window + 1;
+  return b > 0 ? b * v.block : 0;
+}
+__host__ __device__ inline int64_t paged_high(const PagedView& v, int64_t p, int64_t held) {
+  const int64_t e = (p / v.block + 1) * v.block;
+  return e < held ? e : held;
+}
+
+// Key units of the tokens at positions p0..p1 of a sequence that holds `held`:
+// units 0..n_sink-1 cover [0, sinks), the others [from, end).
+struct TileSpan {
+  int32_t n_sink, n_units;
+  int32_t from, end, sinks;
+};
+__host__ __device__ inline TileSpan tile_span(const PagedView& v, int64_t p0, int64_t p1, int64_t held, int unit_keys) {
+  TileSpan t;
+  const int64_t low = paged_low(v, p0) & ~int64_t(63);  // pages of whole 64s are then read from their start
+  t.end = int32_t(paged_high(v, p1, held));
+  if (v.sink_tokens >= low) {
+    t.sinks = 0;
+    t.from = 0;
+  } else {
+    t.sinks = int32_t(v.sink_tokens);
+    t.from = int32_t(low);
+  }
+  t.n_sink = (t.sinks + unit_keys - 1) / unit_keys;
+  t.n_units = t.n_sink + (t.end - t.from + unit_keys - 1) / unit_keys;
+  return t;
+}
+
+struct PagedAttendArgs {
+  PagedView v;
+  const char* q;
+  char* out;
+  float* lse;
+  const char* pages;       // of the layer
+  size_t q_pitch, out_pitch;  // bytes between rows
+  int64_t rows;
+  float scale;
+};
+
+hipError_t launch_paged_attend(const PagedAttendArgs& a, bool bf16, bool narrow, hipStream_t stream);
+
+}  // namespace fademem

@@ -39,7 +39,24 @@ EXPORTED = (
     "fademem_strerror", "fademem_spectral_workspace_bytes", "fademem_spectral_corr", "fademem_stage",
     "fademem_update_staged", "fademem_attend_staged", "fademem_verify", "fademem_spectral_band_map",
     "fademem_spectral_horizons", "fademem_spectral_fit", "fademem_spectral_corr_static",
+    "fademem_rope_init", "fademem_rope_apply", "fademem_paged_bytes", "fademem_paged_create",
+    "fademem_paged_destroy", "fademem_paged_plan", "fademem_paged_array", "fademem_paged_insert",
+    "fademem_paged_attend", "fademem_paged_last_hip_error",
 )
+
+FADEMEM_ROPE_INTERLEAVED = 0
+FADEMEM_ROPE_HALVES = 1
+FADEMEM_ROPE_MAX_PAIRS = 128
+ROPE_LAYOUTS = {"interleaved": FADEMEM_ROPE_INTERLEAVED, "halves": FADEMEM_ROPE_HALVES}
+
+FADEMEM_PAGED_Q_START = 0
+FADEMEM_PAGED_SLOTS = 1
+FADEMEM_PAGED_POSITIONS = 2
+FADEMEM_PAGED_STATUS = 3
+FADEMEM_PAGED_HELD = 4
+FADEMEM_PAGED_TABLE = 5
+FADEMEM_PAGED_FREE = 6
+FADEMEM_PAGED_PAGES = 7
 
 
 class fademem_config(ctypes.Structure):
@@ -56,6 +73,35 @@ class fademem_config(ctypes.Structure):
         ("rope_pairs", ctypes.c_int32),
         ("rope_theta", ctypes.c_double),
         ("stage_frames", ctypes.c_int32),
+    ]
+
+
+class fademem_rope(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+        ("pairs", ctypes.c_int32 * 3),
+        ("freq", ctypes.c_double * FADEMEM_ROPE_MAX_PAIRS),
+    ]
+
+
+class fademem_paged_config(ctypes.Structure):
+    _fields_ = [
+        ("seqs", ctypes.c_int32),
+        ("layers", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("sinks", ctypes.c_int32),
+        ("pages", ctypes.c_int64),
+        ("max_tokens", ctypes.c_int64),
+        ("max_rows", ctypes.c_int64),
+        ("block_tokens", ctypes.c_int64),
+        ("window", ctypes.c_int64),
+        ("grid_h", ctypes.c_int32),
+        ("grid_w", ctypes.c_int32),
     ]
 
 
@@ -127,6 +173,18 @@ def lib() -> ctypes.CDLL:
     L.fademem_spectral_fit.argtypes = [c_void_p, c_void_p, c_int64, c_int32, P(ctypes.c_double),
                                        P(ctypes.c_double)]
     L.fademem_last_hip_error.argtypes = [c_void_p]
+    L.fademem_rope_init.argtypes = [P(fademem_rope), c_int32, c_int32, c_int32, c_int32, c_int32, ctypes.c_double]
+    L.fademem_rope_apply.argtypes = [P(fademem_rope), c_int32, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p,
+                                     c_int64, c_int32, c_void_p]
+    L.fademem_paged_bytes.argtypes = [P(fademem_paged_config), P(ctypes.c_size_t)]
+    L.fademem_paged_create.argtypes = [P(fademem_paged_config), c_void_p, ctypes.c_size_t, c_void_p, P(c_void_p)]
+    L.fademem_paged_destroy.argtypes = [c_void_p]
+    L.fademem_paged_plan.argtypes = [c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_void_p]
+    L.fademem_paged_array.argtypes = [c_void_p, c_int32, c_int32, P(c_void_p), P(c_int64)]
+    L.fademem_paged_insert.argtypes = [c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_int64, P(fademem_rope), c_void_p]
+    L.fademem_paged_attend.argtypes = [c_void_p, c_int32, c_void_p, c_int64, ctypes.c_float, c_void_p, c_int64, c_void_p,
+                                       c_void_p]
+    L.fademem_paged_last_hip_error.argtypes = [c_void_p]
     for name in EXPORTED:
         if name != "fademem_strerror":
             getattr(L, name).restype = c_int
@@ -309,6 +367,63 @@ def fademem_spectral_fit(t_ptr: int, r_ptr: int, n: int, iters: int = 100):
     _ok(lib().fademem_spectral_fit(ctypes.c_void_p(t_ptr), ctypes.c_void_p(r_ptr), n, iters, ctypes.byref(a),
                                    ctypes.byref(b)), "fademem_spectral_fit")
     return a.value, b.value
+
+
+def fademem_rope_init(head_dim: int, layout: int, pairs_t: int, pairs_h: int, pairs_w: int,
+                      theta: float) -> fademem_rope:
+    rope = fademem_rope()
+    _ok(lib().fademem_rope_init(ctypes.byref(rope), head_dim, layout, pairs_t, pairs_h, pairs_w, theta),
+        "fademem_rope_init")
+    return rope
+
+
+def fademem_rope_apply(rope: fademem_rope, dtype: int, pos_ptr: int, rows: int, heads: int, x_ptr: int, x_stride: int,
+                       y_ptr: int, y_stride: int, inverse: int = 0, stream: int = 0) -> None:
+    _ok(lib().fademem_rope_apply(rope, dtype, pos_ptr, rows, heads, x_ptr, x_stride, y_ptr, y_stride, inverse, stream),
+        "fademem_rope_apply")
+
+
+def fademem_paged_bytes(cfg: fademem_paged_config) -> int:
+    n = ctypes.c_size_t(0)
+    _ok(lib().fademem_paged_bytes(cfg, ctypes.byref(n)), "fademem_paged_bytes")
+    return n.value
+
+
+def fademem_paged_create(cfg: fademem_paged_config, pool_ptr: int, pool_bytes: int, stream: int = 0) -> int:
+    h = ctypes.c_void_p(0)
+    _ok(lib().fademem_paged_create(cfg, pool_ptr, pool_bytes, stream, ctypes.byref(h)), "fademem_paged_create")
+    return h.value
+
+
+def fademem_paged_destroy(handle: int) -> None:
+    _ok(lib().fademem_paged_destroy(handle), "fademem_paged_destroy")
+
+
+def fademem_paged_plan(handle: int, kept_ptr: int, added_ptr: int, rows: int, max_new: int, stream: int = 0) -> None:
+    _ok(lib().fademem_paged_plan(handle, kept_ptr, added_ptr, rows, max_new, stream), "fademem_paged_plan")
+
+
+def fademem_paged_array(handle: int, which: int, layer: int = 0):
+    """(device address, elements) of one of the store's arrays."""
+    p, n = ctypes.c_void_p(0), ctypes.c_int64(0)
+    _ok(lib().fademem_paged_array(handle, which, layer, ctypes.byref(p), ctypes.byref(n)), "fademem_paged_array")
+    return p.value, n.value
+
+
+def fademem_paged_insert(handle: int, layer: int, k_ptr: int, k_stride: int, v_ptr: int, v_stride: int,
+                         rope: Optional[fademem_rope] = None, stream: int = 0) -> None:
+    _ok(lib().fademem_paged_insert(handle, layer, k_ptr, k_stride, v_ptr, v_stride, rope, stream),
+        "fademem_paged_insert")
+
+
+def fademem_paged_attend(handle: int, layer: int, q_ptr: int, q_stride: int, scale: float, out_ptr: int,
+                         out_stride: int, lse_ptr: int = 0, stream: int = 0) -> None:
+    _ok(lib().fademem_paged_attend(handle, layer, q_ptr, q_stride, scale, out_ptr, out_stride, lse_ptr, stream),
+        "fademem_paged_attend")
+
+
+def fademem_paged_last_hip_error(handle: int) -> int:
+    return lib().fademem_paged_last_hip_error(handle)
 
 
 def fademem_last_hip_error(handle: int) -> int:

@@ -1,0 +1,72 @@
+"""Rotary positions with a time, a height and a width axis.
+
+Argument marshalling for fademem_rope_apply (include/fademem.h): the rotation
+of a chunk's queries and keys, and its inverse, which is its gradient.
+"""
+from __future__ import annotations
+
+from typing import Optional, Sequence
+
+from . import fademem as fm
+
+
+def rows_of(t, name: str, dtype, device, heads: Optional[int] = None, head_dim: Optional[int] = None,
+            rows: Optional[int] = None) -> int:
+    """Checks a [rows][heads][head_dim] tensor whose heads and elements are
+    contiguous (rows may be apart) and returns its elements between rows."""
+    if t.dtype != dtype or not t.is_cuda or t.device != device or t.dim() != 3:
+        raise ValueError(f"{name}: expected a [rows][heads][head_dim] {dtype} tensor on {device}")
+    if (heads is not None and t.shape[1] != heads) or (head_dim is not None and t.shape[2] != head_dim):
+        raise ValueError(f"{name}: expected [rows][{heads}][{head_dim}]")
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name}: expected {rows} rows")
+    row = t.shape[1] * t.shape[2]
+    if t.numel() == 0:
+        return row
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name}: heads and elements must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else row
+
+
+class Rotary:
+    """A rotation: `pairs` = (time, height, width) pairs of a head, in this
+    order from its first pair on (the rest is copied); pair k of an axis with
+    P pairs turns by theta^(-k/P) per position.  layout: "interleaved" (pair p
+    is elements 2p, 2p+1) or "halves" (p, p + head_dim/2).  `freq`, if given,
+    replaces the frequencies (one per pair)."""
+
+    def __init__(self, head_dim: int, pairs: Sequence[int], theta: float = 10000.0, layout: str = "interleaved",
+                 freq: Optional[Sequence[float]] = None):
+        if layout not in fm.ROPE_LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(fm.ROPE_LAYOUTS)}")
+        if len(pairs) != 3:
+            raise ValueError("pairs: expected three numbers (time, height, width)")
+        self.head_dim, self.pairs, self.layout = int(head_dim), tuple(int(p) for p in pairs), layout
+        self.rope = fm.fademem_rope_init(self.head_dim, fm.ROPE_LAYOUTS[layout], *self.pairs, theta)
+        if freq is not None:
+            if len(freq) != sum(self.pairs):
+                raise ValueError(f"freq: expected {sum(self.pairs)} frequencies")
+            for i, f in enumerate(freq):
+                self.rope.freq[i] = float(f)
+
+    def apply(self, x, pos, out=None, inverse: bool = False, stream=None):
+        """x [rows][heads][head_dim] (float32 or bfloat16; rows may be apart,
+        as in a joint projection's output) turned to the positions pos, a
+        contiguous int32 [rows][3] tensor of (time, height, width).  out may be
+        x.  inverse=True turns back: the gradient of apply."""
+        import torch
+        if x.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("x: expected float32 or bfloat16")
+        x_stride = rows_of(x, "x", x.dtype, x.device, head_dim=self.head_dim,
+                           heads=x.shape[1] if x.dim() == 3 else None)
+        rows, heads = x.shape[0], x.shape[1]
+        if pos.dtype != torch.int32 or tuple(pos.shape) != (rows, 3) or not pos.is_contiguous() or pos.device != x.device:
+            raise ValueError(f"pos: expected a contiguous int32 [{rows}][3] tensor on {x.device}")
+        if out is None:
+            out = torch.empty((rows, heads, self.head_dim), dtype=x.dtype, device=x.device)
+        y_stride = rows_of(out, "out", x.dtype, x.device, heads, self.head_dim, rows)
+        with torch.cuda.device(x.device):
+            fm.fademem_rope_apply(self.rope, fm.FADEMEM_BF16 if x.dtype == torch.bfloat16 else fm.FADEMEM_F32,
+                                  pos.data_ptr(), rows, heads, x.data_ptr(), x_stride, out.data_ptr(), y_stride,
+                                  int(inverse), fm.current_stream() if stream is None else int(stream.cuda_stream))
+        return out
