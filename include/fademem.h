@@ -443,8 +443,8 @@ typedef struct fademem_paged_config {
 typedef struct fademem_paged fademem_paged; /* opaque host object */
 
 /* Bytes of device pool: tables, the step's plan, the attention's scratch for
- * split work, and per layer [pages][K|V][kv_heads][page_tokens][head_dim].
- * Errors: EINVAL. */
+ * split work, and per layer [pages][K|V][kv_heads][page_tokens][head_dim]
+ * (one page of K and V: 2 GiB at most).  Errors: EINVAL. */
 int fademem_paged_bytes(const fademem_paged_config* cfg, size_t* bytes);
 
 /* Create a store over a caller-owned pool (256-byte aligned); every sequence

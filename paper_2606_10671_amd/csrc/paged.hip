@@ -76,7 +76,7 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   const unsigned __int128 seqs = unsigned(c.seqs);
   const unsigned __int128 page = (unsigned __int128)2 * unsigned(c.kv_heads) * uint64_t(P) * unsigned(c.head_dim) * elt;
   const unsigned __int128 layer = page * uint64_t(c.pages);
-  if (layer * unsigned(c.layers) > kMaxPool || seqs * uint64_t(width) * 4 > kMaxPool) return false;
+  if (page > (uint64_t(1) << 31) || layer * unsigned(c.layers) > kMaxPool || seqs * uint64_t(width) * 4 > kMaxPool) return false;
   const TileShape wide = c.dtype == FADEMEM_BF16 ? kPagedWideBf16 : kPagedWideF32;
   v->pool = pool;
   v->header = reinterpret_cast<PagedHeader*>(take(sizeof(PagedHeader)));
@@ -93,17 +93,17 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   v->tile0 = reinterpret_cast<int32_t*>(take((seqs + 1) * 4));
   v->unit_end = reinterpret_cast<int64_t*>(take(uint64_t(max_tiles(c)) * 8));
   v->starts = reinterpret_cast<WorkStart*>(take((kPagedMaxGroups + 1) * sizeof(WorkStart)));
-  v->redo = reinterpret_cast<uint8_t*>(take((unsigned __int128)uint64_t(max_tiles(c)) * unsigned(c.kv_heads) * 8));
+  v->redo = reinterpret_cast<uint64_t*>(take((unsigned __int128)uint64_t(max_tiles(c)) * unsigned(c.kv_heads) * 8));
   v->scratch = reinterpret_cast<float*>(take(2 * kPagedMaxGroups * paged_slot_floats(wide.rows, c.head_dim) * 4));
   v->pages = take(layer * unsigned(c.layers));
-  v->page_bytes = size_t(page);
+  v->page_bytes = uint32_t(page);
   v->layer_bytes = size_t(layer);
   v->n_pages = c.pages;
   v->max_tokens = c.max_tokens;
-  v->block = c.block_tokens;
-  v->window = c.window;
+  v->block = int32_t(c.block_tokens);
+  v->window = int32_t(c.window);
   const int64_t most = int64_t(1) << 30;  // beyond every sequence
-  v->sink_tokens = c.window == 0 ? 0 : c.sinks > most / c.block_tokens ? most : int64_t(c.sinks) * c.block_tokens;
+  v->sink_tokens = int32_t(c.window == 0 ? 0 : c.sinks > most / c.block_tokens ? most : c.sinks * c.block_tokens);
   v->seqs = c.seqs;
   v->heads = c.heads;
   v->kv_heads = c.kv_heads;
@@ -112,6 +112,11 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   v->page_tokens = int32_t(P);
   v->width = int32_t(width);
   v->front = int32_t((v->sink_tokens + P - 1) / P);
+  // 2^(30+L) / P rounded up, 2^L >= P: the product is off by less than key / 2^(30+L) < 1/P.
+  int shift = 30;
+  while ((int64_t(1) << (shift - 30)) < P) ++shift;
+  v->page_shift = shift;
+  v->page_magic = uint32_t(((uint64_t(1) << shift) + uint64_t(P) - 1) / uint64_t(P));
   v->grid_h = c.grid_h;
   v->grid_w = c.grid_w;
   if (at > kMaxPool) return false;
@@ -227,7 +232,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   if (k < 0 || n < 0 || n > a.max_new || k > held || k + n > v.max_tokens || (n > 0 && row_end > a.rows))
     code = FADEMEM_EINVAL;
   const int32_t front = v.front;
-  const int64_t low_page = code ? 0 : paged_low(v, k) / P;
+  const int64_t low_page = code ? 0 : paged_low(v, int32_t(k)) / P;
   const bool restart = gone > front && k <= front * P;  // all that is kept lies in the sinks' pages
   if (!code && gone > front && !restart && low_page < gone) code = FADEMEM_ESTATE;
   const bool ok = live && code == FADEMEM_OK;
@@ -361,7 +366,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
       const int q = last_at_most<int64_t>(pre, seqs, t);
       const int64_t row0 = (t - pre[q]) * a.shape.rows, row1 = min(row0 + a.shape.rows, int64_t(r2_lo[q]) * G);
       const int64_t p = r1_lo[q];
-      units = tile_span(v, p + row0 / G, p + (row1 - 1) / G, p + r2_lo[q], a.shape.unit_keys).n_units;
+      units = tile_span(v, int32_t(p + row0 / G), int32_t(p + (row1 - 1) / G), int32_t(p + r2_lo[q]), a.shape.unit_keys).n_units;
     }
     const int64_t end = units0 + block_scan(units, red, &sum);
     if (t < n_tiles) v.unit_end[t] = end;
@@ -489,8 +494,11 @@ __global__ __launch_bounds__(kRotThreads) void paged_insert_kernel(PagedInsertAr
   }
 }
 
-bool narrow_step(const fademem_paged* c) {
-  return c->max_new * c->view.group <= kPagedNarrowBf16.rows;
+// The step's attention kernel: narrow where every sequence's rows fit one narrow tile.
+bool narrow_step(const fademem_paged* c) { return c->max_new * c->view.group <= kPagedNarrowBf16.rows; }
+TileShape step_shape(const fademem_paged* c) {
+  return c->cfg.dtype == FADEMEM_BF16 ? (narrow_step(c) ? kPagedNarrowBf16 : kPagedWideBf16)
+                                      : (narrow_step(c) ? kPagedNarrowF32 : kPagedWideF32);
 }
 
 }  // namespace
@@ -564,11 +572,9 @@ int fademem_paged_plan(fademem_paged* c, const int32_t* kept, const int32_t* add
   a.added = added;
   a.rows = rows;
   a.max_new = max_new;
-  const bool narrow = narrow_step(c);
-  a.shape = c->cfg.dtype == FADEMEM_BF16 ? (narrow ? kPagedNarrowBf16 : kPagedWideBf16)
-                                         : (narrow ? kPagedNarrowF32 : kPagedWideF32);
+  a.shape = step_shape(c);
   a.max_groups = kPagedMaxGroups;
-  a.min_units = narrow ? 1 : 4;
+  a.min_units = narrow_step(c) ? 1 : 4;
   hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, as_stream(stream), a);
   if (rows > 0)
     hipLaunchKernelGGL(paged_rows_kernel, dim3(unsigned((rows + kFillThreads - 1) / kFillThreads)), dim3(kFillThreads), 0,
@@ -670,7 +676,9 @@ int fademem_paged_attend(fademem_paged* c, int32_t layer, const void* q, int64_t
   a.out_pitch = size_t(out_stride) * elt;
   a.rows = c->rows;
   a.scale = scale == 0.0f ? 1.0f / sqrtf(float(c->cfg.head_dim)) : scale;
-  const hipError_t e = launch_paged_attend(a, c->cfg.dtype == FADEMEM_BF16, narrow_step(c), as_stream(stream));
+  const bool bf16 = c->cfg.dtype == FADEMEM_BF16, narrow = narrow_step(c);
+  hipError_t e = bf16 ? launch_paged_bf16(a, narrow, as_stream(stream)) : launch_paged_f32(a, narrow, as_stream(stream));
+  if (e == hipSuccess) e = launch_paged_finish(a, bf16, step_shape(c), as_stream(stream));
   if (e != hipSuccess) return hip_fail(c, e);
   return finish(c, stream);
 }

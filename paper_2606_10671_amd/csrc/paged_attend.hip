@@ -1,16 +1,21 @@
-// Attention of a step's queries over the paged window memory.
+// Paged attention: what follows the kernels of paged_bf16.hip and paged_f32.hip.
 //
-// O = softmax(scale Q K^T) V over the keys that a row sees: the sinks [0, S) and
-// the window [low, high) of its position.
-#include "bf16_round.h"
-#include "paged_internal.h"
+// paged_finish_kernel
+// * joins the partial results of row tiles whose keys several workgroups shared,
+//   in the order of the workgroups: O = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i;
+// * works out again, key by key, rows whose result is not finite.  The matrix
+//   kernels give a hidden key the weight 0, and 0 times an infinite or NaN value
+//   is NaN: such a row is only right if it saw that value.  attend_row adds up
+//   the keys that the row sees and no others;
+// * writes 0 (and an LSE of minus infinity) to the rows of sequences that were
+//   not admitted to the step.
+#include "paged_device.h"
 
 namespace fademem {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kRowWaves = 4;
+constexpr int kFinishThreads = 256;
+constexpr int kFinishWaves = kFinishThreads / 64;
 
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
@@ -23,42 +28,40 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-// Byte address of key (or value) `key` of sequence table `table`, key head hk.
-__device__ __forceinline__ const char* key_row(const PagedAttendArgs& a, const int32_t* table, int key, int hk, int kv,
+// Address of key `key` of a sequence in key head hk's K rows.
+__device__ __forceinline__ const char* key_row(const PagedAttendArgs& a, const int32_t* table, int key, int hk,
                                                int row_bytes) {
-  const int page = key / a.v.page_tokens, off = key - page * a.v.page_tokens;
-  const int32_t id = min(max(table[page], 0), int32_t(a.v.n_pages) - 1);
-  return a.pages + size_t(id) * a.v.page_bytes + (size_t(kv * a.v.kv_heads + hk) * a.v.page_tokens + off) * row_bytes;
+  const int page = page_of(a.v, key), off = key - page * a.v.page_tokens;
+  return a.pages + size_t(safe_page(a.v, table[page])) * a.v.page_bytes +
+         (size_t(hk) * a.v.page_tokens + off) * row_bytes;
 }
 
-// One row of one head by one wave: a lane takes a key of 64, then two (or one)
+// One row of one head by one wave: a lane takes one key of 64, then D/64
 // elements of the output.  q_s: the wave's D floats of LDS.
 template <bool BF16, int D>
-__device__ void attend_row(const PagedAttendArgs& a, int s, int row, int h, float* q_s) {
+__device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, float* q_s) {
   constexpr int kPer = D / 64;  // output elements per lane
   constexpr int kElt = BF16 ? 2 : 4;
   const PagedView& v = a.v;
-  const int lane = threadIdx.x & 63, hk = h / v.group;
-  const char* q = a.q + size_t(row) * a.q_pitch + size_t(h) * D * kElt;
+  const int lane = threadIdx.x & 63, hk = qr.head / v.group;
+  const char* q = a.q + size_t(qr.row) * a.q_pitch + size_t(qr.head) * D * kElt;
   for (int d = lane; d < D; d += 64)
     q_s[d] = BF16 ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(q)[d]) << 16)
                   : reinterpret_cast<const float*>(q)[d];
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
   const int32_t* table = v.table + size_t(s) * v.width;
-  const int pos = v.first[s] + row - v.q_start[s], held = v.held[s];
-  const int low = int(paged_low(v, pos)), high = v.added[s] > 0 ? int(paged_high(v, pos, held)) : 0;
-  const int sinks = int(min(v.sink_tokens, int64_t(min(low, high))));
+  const int sinks = min(v.sink_tokens, min(qr.low, qr.high));
   const float c2 = a.scale * kLog2e;
   float m = -INFINITY, l = 0.0f, o[kPer] = {};
   for (int part = 0; part < 2; ++part) {
-    const int end = part ? high : sinks;
-    for (int k0 = part ? low : 0; k0 < end; k0 += 64) {
+    const int end = part ? qr.high : sinks;
+    for (int k0 = part ? qr.low : 0; k0 < end; k0 += 64) {
       const int key = k0 + lane, n = min(64, end - k0);
       const char* vrow = nullptr;
       float x = -INFINITY;
       if (key < end) {
-        const char* krow = key_row(a, table, key, hk, 0, D * kElt);
+        const char* krow = key_row(a, table, key, hk, D * kElt);
         vrow = krow + size_t(v.kv_heads) * v.page_tokens * D * kElt;
         x = 0.0f;
         for (int d = 0; d < D; d += 16 / kElt) {
@@ -95,44 +98,152 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, int row, int h, floa
           o[e] = __builtin_fmaf(pj, x1, o[e]);
         }
       }
-      if (l != l) k0 = end, part = 2;  // a NaN score: every element is NaN
+      if (l != l) break;  // a NaN score: every element is NaN
     }
+    if (l != l) break;
   }
-  char* out = a.out + size_t(row) * a.out_pitch + size_t(h) * D * kElt;
+  char* out = a.out + size_t(qr.row) * a.out_pitch + size_t(qr.head) * D * kElt;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
-    const float y = l != l ? l : high > 0 ? o[e] / l : 0.0f;
+    const float y = l != l ? l : o[e] / l;
     if constexpr (BF16) reinterpret_cast<__bf16*>(out)[lane * kPer + e] = (__bf16)y;
     else reinterpret_cast<float*>(out)[lane * kPer + e] = y;
   }
-  if (a.lse && lane == 0) a.lse[size_t(h) * a.rows + row] = high > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
+  if (a.lse && lane == 0) a.lse[size_t(qr.head) * a.rows + qr.row] = (m + log2f(l)) * kLn2;
 }
 
+constexpr int kJoinRows = 8;  // rows of a tile that one block joins
+
+// grid = (groups at most, row chunks of a tile).
 template <bool BF16, int D>
-__global__ __launch_bounds__(64 * kRowWaves) void paged_attend_rows_kernel(PagedAttendArgs a) {
-  __shared__ float q_s[kRowWaves][D];
-  const int wave = threadIdx.x >> 6;
-  const int64_t i = int64_t(blockIdx.x) * kRowWaves + wave;
-  const int row = int(i / a.v.heads), h = int(i - int64_t(row) * a.v.heads);
-  if (row >= a.v.q_start[a.v.seqs]) return;
-  int lo = 0, hi = a.v.seqs;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.v.q_start[mid] <= row) lo = mid;
-    else hi = mid;
+__global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAttendArgs a, TileShape shape) {
+  __shared__ float q_s[kFinishWaves][D];
+  __shared__ int list[kFinishThreads], n_list;
+  const PagedView& v = a.v;
+  const int tid = threadIdx.x, wave = tid >> 6, g = blockIdx.x;
+  const int groups = v.header->groups;
+
+  // Join the tile that boundary g is the first to cut.
+  const WorkStart w = g > 0 && g < groups ? v.starts[g] : WorkStart{0, 0, 0, 0};
+  bool first_cut = w.unit > 0;
+  if (first_cut) {
+    const WorkStart b = v.starts[g - 1];
+    first_cut = b.unit == 0 || b.tile != w.tile || b.head != w.head;
   }
-  attend_row<BF16, D>(a, lo, row, h, q_s[wave]);
+  if (first_cut) {
+    Segment s;
+    s.seq = w.seq;
+    s.head = w.head;
+    s.first = v.first[w.seq];
+    s.held = v.held[w.seq];
+    s.q_start = v.q_start[w.seq];
+    s.row0 = (w.tile - v.tile0[w.seq]) * shape.rows;
+    s.rows = min(shape.rows, v.added[w.seq] * v.group - s.row0);
+    constexpr int kLanes = D / 4;  // threads of a row
+    const int r = blockIdx.y * kJoinRows + tid / kLanes, c = 4 * (tid % kLanes);
+    bool bad = false;
+    if (tid < kJoinRows * kLanes && r < s.rows) {
+      // Parts: group g - 1's last units, then the first units of groups g, g+1, ... while they begin in this tile.
+      int parts = 2;
+      while (g + parts - 1 < groups) {
+        const WorkStart x = v.starts[g + parts - 1];
+        if (x.unit == 0 || x.tile != w.tile || x.head != w.head) break;
+        ++parts;
+      }
+      const size_t slot = paged_slot_floats(shape.rows, D);
+      auto part = [&](int p) { return v.scratch + size_t(p == 0 ? 2 * (g - 1) + 1 : 2 * (g + p - 1)) * slot; };
+      const size_t mi = size_t(shape.rows) * D + r, li = mi + shape.rows;
+      float m = -INFINITY;
+#pragma unroll 8
+      for (int p = 0; p < parts; ++p) m = fmaxf(m, part(p)[mi]);
+      const float ref = m == -INFINITY ? 0.0f : m;
+      float l = 0.0f, o[4] = {};
+#pragma unroll 8
+      for (int p = 0; p < parts; ++p) {
+        const float* x = part(p);
+        const float f = exp2f(x[mi] - ref);
+        const float4 y = *reinterpret_cast<const float4*>(x + size_t(r) * D + c);
+        l += f * x[li];
+        o[0] += f * y.x;
+        o[1] += f * y.y;
+        o[2] += f * y.z;
+        o[3] += f * y.w;
+      }
+      const QueryRow q = query_row(v, s, r);
+      const float inv = 1.0f / l;
+      char* out = a.out + size_t(q.row) * a.out_pitch + (size_t(q.head) * D + c) * (BF16 ? 2 : 4);
+      if constexpr (BF16) {
+        uint2 y = {round_pair(o[0] * inv, o[1] * inv), round_pair(o[2] * inv, o[3] * inv)};
+        *reinterpret_cast<uint2*>(out) = y;
+      } else {
+        *reinterpret_cast<float4*>(out) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+      }
+      if (a.lse && c == 0) a.lse[size_t(q.head) * a.rows + q.row] = (m + log2f(l)) * kLn2;
+      const float sum = (o[0] + o[1]) + (o[2] + o[3]) + inv;
+      bad = !(fabsf(sum) < INFINITY);
+    }
+    if (__syncthreads_or(bad))
+      for (int i = wave; i < kJoinRows; i += kFinishWaves)
+        if (int(blockIdx.y) * kJoinRows + i < s.rows)
+          attend_row<BF16, D>(a, s.seq, query_row(v, s, blockIdx.y * kJoinRows + i), q_s[wave]);
+  }
+  if (blockIdx.y > 0) return;
+
+  // Rows of tiles that one workgroup finished, marked by it.
+  const int64_t jobs = int64_t(v.tile0[v.seqs]) * v.kv_heads;
+  for (int64_t j0 = int64_t(g) * kFinishThreads; j0 < jobs; j0 += int64_t(gridDim.x) * kFinishThreads) {
+    const uint64_t mark = j0 + tid < jobs ? v.redo[j0 + tid] : 0;
+    if (!__syncthreads_or(mark != 0)) continue;
+    if (tid == 0) n_list = 0;
+    __syncthreads();
+    if (mark) list[atomicAdd(&n_list, 1)] = tid;
+    __syncthreads();
+    for (int i = 0; i < n_list; ++i) {
+      const int64_t j = j0 + list[i];
+      const uint64_t marks = v.redo[j];
+      const int tile = int(j / v.kv_heads);
+      int lo = 0, hi = v.seqs;  // the last sequence whose tiles begin at or before it
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (v.tile0[mid] <= tile) lo = mid;
+        else hi = mid;
+      }
+      Segment s;
+      s.seq = lo;
+      s.head = int(j - int64_t(tile) * v.kv_heads);
+      s.first = v.first[lo];
+      s.held = v.held[lo];
+      s.q_start = v.q_start[lo];
+      s.row0 = (tile - v.tile0[lo]) * shape.rows;
+      s.rows = min(shape.rows, v.added[lo] * v.group - s.row0);
+      for (int r = wave; r < s.rows; r += kFinishWaves)
+        if ((marks >> (8 * (r >> 5))) & 0xff) attend_row<BF16, D>(a, lo, query_row(v, s, r), q_s[wave]);
+    }
+    __syncthreads();
+  }
+
+  // Rows of sequences that were not admitted.
+  for (int s = g; s < v.seqs; s += gridDim.x) {
+    if (v.status[s] == FADEMEM_OK) continue;
+    const int r0 = v.q_start[s], r1 = v.q_start[s + 1];
+    const int units = v.heads * D * (BF16 ? 2 : 4) / 16;
+    for (int64_t i = tid; i < int64_t(r1 - r0) * units; i += kFinishThreads) {
+      const int64_t row = r0 + i / units;
+      reinterpret_cast<uint4*>(a.out + size_t(row) * a.out_pitch)[i % units] = make_uint4(0, 0, 0, 0);
+    }
+    if (a.lse)
+      for (int64_t i = tid; i < int64_t(r1 - r0) * v.heads; i += kFinishThreads)
+        a.lse[(i / (r1 - r0)) * a.rows + r0 + i % (r1 - r0)] = -INFINITY;
+  }
 }
 
 }  // namespace
 
-hipError_t launch_paged_attend(const PagedAttendArgs& a, bool bf16, bool narrow, hipStream_t stream) {
-  (void)narrow;
-  auto kernel = a.v.head_dim == 128 ? (bf16 ? paged_attend_rows_kernel<true, 128> : paged_attend_rows_kernel<false, 128>)
-                                    : (bf16 ? paged_attend_rows_kernel<true, 64> : paged_attend_rows_kernel<false, 64>);
-  const int64_t blocks = (a.rows * a.v.heads + kRowWaves - 1) / kRowWaves;
-  if (blocks > int64_t(0x7fffffff)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(64 * kRowWaves), 0, stream, a);
+hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, hipStream_t stream) {
+  auto kernel = a.v.head_dim == 128 ? (bf16 ? paged_finish_kernel<true, 128> : paged_finish_kernel<false, 128>)
+                                    : (bf16 ? paged_finish_kernel<true, 64> : paged_finish_kernel<false, 64>);
+  hipLaunchKernelGGL(kernel, dim3(kPagedMaxGroups, unsigned(shape.rows / kJoinRows)), dim3(kFinishThreads), 0, stream, a,
+                     shape);
   return hipGetLastError();
 }
 

@@ -64,50 +64,49 @@ struct PagedView {
   int32_t* tile0;      // [seqs + 1] first row tile of each sequence
   int64_t* unit_end;   // [tiles] units of one head up to and with each tile
   WorkStart* starts;   // [groups + 1]
-  uint8_t* redo;       // [tiles][kv_heads][8]: the rows of a tile's wave have to be worked out again
+  uint64_t* redo;      // [tiles][kv_heads]: byte w != 0: rows 32 w.. of the tile have to be worked out again
   float* scratch;      // attention partials
   char* pages;         // layer 0
   size_t layer_bytes;
-  size_t page_bytes;
   int64_t n_pages;
   int64_t max_tokens;
-  int64_t block;       // B
-  int64_t window;      // W, 0: everything
-  int64_t sink_tokens; // S * B (0 without a window)
+  uint32_t page_bytes;
+  int32_t block;       // B
+  int32_t window;      // W, 0: everything
+  int32_t sink_tokens; // S * B (0 without a window)
   int32_t seqs, heads, kv_heads, group, head_dim;
   int32_t page_tokens, width;
   int32_t front;       // pages that hold sinks
   int32_t grid_h, grid_w;
+  uint32_t page_magic;  // key / page_tokens = key * page_magic >> page_shift for keys below 2^30
+  int32_t page_shift;
 };
 
 // First key of the window of a query at position p, and the end of what it sees.
-__host__ __device__ inline int64_t paged_low(const PagedView& v, int64_t p) {
+__host__ __device__ inline int32_t paged_low(const PagedView& v, int32_t p) {
   if (v.window == 0) return 0;
-  const int64_t b = p / v.block - v.window + 1;
+  const int32_t b = int32_t(uint32_t(p) / uint32_t(v.block)) - v.window + 1;
   return b > 0 ? b * v.block : 0;
 }
-__host__ __device__ inline int64_t paged_high(const PagedView& v, int64_t p, int64_t held) {
-  const int64_t e = (p / v.block + 1) * v.block;
-  return e < held ? e : held;
+__host__ __device__ inline int32_t paged_high(const PagedView& v, int32_t p, int32_t held) {
+  const uint32_t e = (uint32_t(p) / uint32_t(v.block) + 1u) * uint32_t(v.block);  // at most p + block, below 2^31
+  return e < uint32_t(held) ? int32_t(e) : held;
 }
 
 // Key units of the tokens at positions p0..p1 of a sequence that holds `held`:
-// units 0..n_sink-1 cover [0, sinks), the others [from, end).
+// units 0..n_sink-1 cover [0, sinks), the others [from, end).  Where the sinks
+// reach the window, one range from 0 covers both.
 struct TileSpan {
   int32_t n_sink, n_units;
   int32_t from, end, sinks;
 };
-__host__ __device__ inline TileSpan tile_span(const PagedView& v, int64_t p0, int64_t p1, int64_t held, int unit_keys) {
+__host__ __device__ inline TileSpan tile_span(const PagedView& v, int32_t p0, int32_t p1, int32_t held, int unit_keys) {
   TileSpan t;
-  const int64_t low = paged_low(v, p0) & ~int64_t(63);  // pages of whole 64s are then read from their start
-  t.end = int32_t(paged_high(v, p1, held));
-  if (v.sink_tokens >= low) {
-    t.sinks = 0;
-    t.from = 0;
-  } else {
-    t.sinks = int32_t(v.sink_tokens);
-    t.from = int32_t(low);
-  }
+  const int32_t low = paged_low(v, p0) & ~63;  // pages of whole 64s are then read from a whole 64 on
+  t.end = paged_high(v, p1, held);
+  const bool apart = v.sink_tokens < low;
+  t.sinks = apart ? v.sink_tokens : 0;
+  t.from = apart ? low : 0;
   t.n_sink = (t.sinks + unit_keys - 1) / unit_keys;
   t.n_units = t.n_sink + (t.end - t.from + unit_keys - 1) / unit_keys;
   return t;
@@ -124,6 +123,11 @@ struct PagedAttendArgs {
   float scale;
 };
 
-hipError_t launch_paged_attend(const PagedAttendArgs& a, bool bf16, bool narrow, hipStream_t stream);
+// Attention of one kernel shape (paged_bf16.hip, paged_f32.hip), and the
+// kernel behind it that joins what workgroups shared and works out again what
+// an infinity or NaN of a hidden key may have reached (paged_attend.hip).
+hipError_t launch_paged_bf16(const PagedAttendArgs& a, bool narrow, hipStream_t stream);
+hipError_t launch_paged_f32(const PagedAttendArgs& a, bool narrow, hipStream_t stream);
+hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, hipStream_t stream);
 
 }  // namespace fademem
