@@ -78,6 +78,7 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   const unsigned __int128 layer = page * uint64_t(c.pages);
   if (page > (uint64_t(1) << 31) || layer * unsigned(c.layers) > kMaxPool || seqs * uint64_t(width) * 4 > kMaxPool) return false;
   const TileShape wide = c.dtype == FADEMEM_BF16 ? kPagedWideBf16 : kPagedWideF32;
+  const TileShape narrow = c.dtype == FADEMEM_BF16 ? kPagedNarrowBf16 : kPagedNarrowF32;
   v->pool = pool;
   v->header = reinterpret_cast<PagedHeader*>(take(sizeof(PagedHeader)));
   v->held = reinterpret_cast<int32_t*>(take(seqs * 4));
@@ -91,10 +92,13 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   v->slots = reinterpret_cast<int64_t*>(take(uint64_t(c.max_rows) * 8));
   v->pos = reinterpret_cast<int32_t*>(take(uint64_t(c.max_rows) * 12));
   v->tile0 = reinterpret_cast<int32_t*>(take((seqs + 1) * 4));
-  v->unit_end = reinterpret_cast<int64_t*>(take(uint64_t(max_tiles(c)) * 8));
+  v->cost_end = reinterpret_cast<int64_t*>(take(uint64_t(max_tiles(c)) * 8));
   v->starts = reinterpret_cast<WorkStart*>(take((kPagedMaxGroups + 1) * sizeof(WorkStart)));
+  v->joins = reinterpret_cast<int32_t*>(take(kPagedMaxGroups * sizeof(int32_t)));
   v->redo = reinterpret_cast<uint64_t*>(take((unsigned __int128)uint64_t(max_tiles(c)) * unsigned(c.kv_heads) * 8));
-  v->scratch = reinterpret_cast<float*>(take(2 * kPagedMaxGroups * paged_slot_floats(wide.rows, c.head_dim) * 4));
+  const size_t wide_slots = 2 * size_t(wide.groups) * paged_slot_floats(wide.rows, c.head_dim);
+  const size_t narrow_slots = 2 * size_t(narrow.groups) * paged_slot_floats(narrow.rows, c.head_dim);
+  v->scratch = reinterpret_cast<float*>(take((wide_slots > narrow_slots ? wide_slots : narrow_slots) * 4));
   v->pages = take(layer * unsigned(c.layers));
   v->page_bytes = uint32_t(page);
   v->layer_bytes = size_t(layer);
@@ -163,27 +167,40 @@ __global__ void paged_init_kernel(PagedView v, int64_t words, int64_t entries) {
 }
 
 constexpr int kPlanThreads = 1024;
+constexpr int64_t kFillInPlan = 4 * kPlanThreads;  // rows up to which the plan's block fills them itself
 constexpr int kPlanWaves = kPlanThreads / 64;
 
-// Inclusive prefix sum over the block; `total` gets the sum.
-__device__ int64_t block_scan(int64_t x, int64_t* red, int64_t* total) {
+// Inclusive prefix sums of N values over the block, in place; total[] gets the
+// sums.  red: N * kPlanWaves values of LDS.
+template <int N>
+__device__ __forceinline__ void block_scan(int64_t (&x)[N], int64_t* red, int64_t (&total)[N]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 63) red[wave] = x;
-  __syncthreads();
-  int64_t before = 0, sum = 0;
+    int64_t y[N];
 #pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) {
-    if (w < wave) before += red[w];
-    sum += red[w];
+    for (int i = 0; i < N; ++i) y[i] = __shfl_up(x[i], o);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += lane >= o ? y[i] : 0;
+  }
+  __syncthreads();  // the last call's sums have been read
+  if (lane == 63) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[i * kPlanWaves + wave] = x[i];
   }
   __syncthreads();
-  *total = sum;
-  return before + x;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    int64_t before = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < kPlanWaves; ++w) {
+      const int64_t y = red[i * kPlanWaves + w];
+      before += w < wave ? y : 0;
+      sum += y;
+    }
+    x[i] += before;
+    total[i] = sum;
+  }
 }
 
 // Last i in [0, n) with a[i] <= x (a[0] <= x, a not decreasing).
@@ -205,31 +222,54 @@ struct PlanArgs {
   int64_t rows, max_new;
   TileShape shape;
   int max_groups;
-  int min_units;  // units of a workgroup at least
+  int min_cost;   // key units (a tile's overhead among them) of a workgroup at least
+  int overhead;   // key units that a tile costs beside its own
+  int fill;       // 1: this kernel also writes the rows' slots and positions
 };
+
+// Slot and position of row i, o tokens behind the sequence's first new one.
+__device__ __forceinline__ void write_row(const PagedView& v, int64_t i, bool live, int s, int32_t p) {
+  int64_t slot = -1;
+  int32_t t = 0, y = 0, x = 0;
+  if (live) {
+    const int32_t frame = v.grid_h * v.grid_w, page = p / v.page_tokens;
+    slot = int64_t(v.table[size_t(s) * v.width + page]) * v.page_tokens + (p - page * v.page_tokens);
+    t = p / frame;
+    y = (p - t * frame) / v.grid_w;
+    x = p - t * frame - y * v.grid_w;
+  }
+  v.slots[i] = slot;
+  v.pos[3 * i] = t;
+  v.pos[3 * i + 1] = y;
+  v.pos[3 * i + 2] = x;
+}
 
 // The step's plan, one block: thread s has sequence s.  What each sequence gives
 // back and needs follows from its lengths alone; prefix sums over the sequences
 // say where its rows, pages and row tiles begin.  Pages are bits of a map, so
 // "the lowest free page" does not depend on the order in which pages came back.
+// Bound by latency: the chain is lengths -> two prefix sums -> pages -> two
+// prefix sums over the row tiles -> the workgroups' starts.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   const PagedView& v = a.v;
-  __shared__ int64_t red[kPlanWaves];
+  __shared__ int64_t red[2 * kPlanWaves];
   __shared__ int64_t pre[kPagedMaxSeqs + 1];  // prefix sums of what the phase deals out
   __shared__ int32_t r1_lo[kPagedMaxSeqs], r1_n[kPagedMaxSeqs], r2_lo[kPagedMaxSeqs];
+  __shared__ int32_t row_start[kPagedMaxSeqs + 1];
+  __shared__ WorkStart starts[kPagedMaxGroups + 1];
   const int tid = threadIdx.x, s = tid, seqs = v.seqs;
   const bool live = s < seqs;
   const int64_t P = v.page_tokens;
-  int64_t total;
+  const int64_t free0 = v.header->free;
 
   // Lengths, checked.
   const int64_t k = live ? a.kept[s] : 0, n = live ? a.added[s] : 0, held = live ? v.held[s] : 0;
   const int32_t gone = live ? v.gone[s] : 0;
   const int64_t want_rows = live && n > 0 ? n : 0;
-  const int64_t row_end = block_scan(want_rows, red, &total);
-  const int64_t row_total = total;
+  int64_t row_end[1] = {want_rows}, row_total[1];
+  block_scan<1>(row_end, red, row_total);
   int32_t code = FADEMEM_OK;
-  if (k < 0 || n < 0 || n > a.max_new || k > held || k + n > v.max_tokens || (n > 0 && row_end > a.rows))
+  if (k < 0 || n < 0 || n > a.max_new || k > held || k + n > v.max_tokens || (n > 0 && row_end[0] > a.rows))
     code = FADEMEM_EINVAL;
   const int32_t front = v.front;
   const int64_t low_page = code ? 0 : paged_low(v, int32_t(k)) / P;
@@ -261,22 +301,24 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
     need = max(0, np - from);
   };
   pages_for(n);
-  const int64_t free0 = v.header->free;
-  block_scan(n1 + n2, red, &total);
-  const int64_t avail = free0 + total;
-  const int64_t need_end = block_scan(need, red, &total);
-  if (ok && need > 0 && need_end > avail) {
-    code = FADEMEM_ENOMEM;
-    pages_for(0);
+  int64_t end[2] = {int64_t(n1) + n2, need}, sum[2];
+  block_scan<2>(end, red, sum);
+  if (sum[1] > free0 + sum[0]) {  // not all fit: the sequences behind the first that does not stay as they are
+    if (ok && need > 0 && end[1] > free0 + sum[0]) {
+      code = FADEMEM_ENOMEM;
+      pages_for(0);
+    }
+    end[0] = int64_t(n1) + n2;
+    end[1] = need;
+    block_scan<2>(end, red, sum);
   }
   const bool admitted = ok && code == FADEMEM_OK;
+  const int64_t released = sum[0], given = sum[1];
 
   // Release.
-  int64_t released;
-  {
-    const int64_t end = block_scan(n1 + n2, red, &released);
+  if (released > 0) {
     if (live) {
-      pre[s] = end - n1 - n2;
+      pre[s] = end[0] - n1 - n2;
       r1_lo[s] = lo1;
       r1_n[s] = n1;
       r2_lo[s] = lo2;
@@ -295,11 +337,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   }
 
   // Allocation: the i-th lowest free page is the i-th needed one.
-  int64_t given;
-  {
-    const int64_t end = block_scan(need, red, &given);
+  if (given > 0) {
     if (live) {
-      pre[s] = end - need;
+      pre[s] = end[1] - need;
       r1_lo[s] = from;
     }
     __syncthreads();
@@ -308,9 +348,10 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
     for (int64_t w0 = 0; w0 < words && rank0 < given; w0 += kPlanThreads) {
       const int64_t w = w0 + tid;
       uint32_t bits = w < words ? __hip_atomic_load(v.bitmap + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
-      int64_t found;
       const int cnt = __popc(bits);
-      int64_t rank = rank0 + block_scan(cnt, red, &found) - cnt;
+      int64_t upto[1] = {cnt}, found[1];
+      block_scan<1>(upto, red, found);
+      int64_t rank = rank0 + upto[0] - cnt;
       const uint32_t before = bits;
       while (bits && rank < given) {
         const int b = __ffs(bits) - 1;
@@ -320,68 +361,72 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
         ++rank;
       }
       if (bits != before) __hip_atomic_store(v.bitmap + w, bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      rank0 += found;
+      rank0 += found[0];
     }
     __syncthreads();
   }
 
   // State.
   const int64_t fresh = admitted ? n : 0;
+  const int32_t row0 = int32_t(min(row_end[0] - want_rows, a.rows)), row_last = int32_t(min(row_total[0], a.rows));
   if (live) {
     v.status[s] = code;
     v.first[s] = int32_t(ok ? k : 0);
     v.added[s] = int32_t(fresh);
-    v.q_start[s] = int32_t(min(row_end - want_rows, a.rows));
+    v.q_start[s] = row0;
     if (ok) {
       v.held[s] = int32_t(k + fresh);
       v.gone[s] = top;
     }
   }
   if (tid == 0) {
-    v.q_start[seqs] = int32_t(min(row_total, a.rows));
+    v.q_start[seqs] = row_last;
     v.header->free = int32_t(free0 + released - given);
   }
 
-  // The attention's work: row tiles, their key units, where each workgroup starts.
+  // The attention's work: row tiles, their costs in key units, where each workgroup starts.
   const int G = v.group;
   const int tiles_s = int((fresh * G + a.shape.rows - 1) / a.shape.rows);
-  int64_t n_tiles;
-  const int64_t tile_end = block_scan(tiles_s, red, &n_tiles);
+  int64_t tile_end[1] = {tiles_s}, n_tiles[1];
+  block_scan<1>(tile_end, red, n_tiles);
   if (live) {
-    pre[s] = tile_end - tiles_s;
-    v.tile0[s] = int32_t(tile_end - tiles_s);
+    pre[s] = tile_end[0] - tiles_s;
+    v.tile0[s] = int32_t(tile_end[0] - tiles_s);
     r1_lo[s] = int32_t(k);
     r2_lo[s] = int32_t(fresh);
+    row_start[s] = row0;
   }
   if (tid == 0) {
-    pre[seqs] = n_tiles;
-    v.tile0[seqs] = int32_t(n_tiles);
+    pre[seqs] = n_tiles[0];
+    v.tile0[seqs] = int32_t(n_tiles[0]);
+    row_start[seqs] = row_last;
   }
   __syncthreads();
-  int64_t units0 = 0;
-  for (int64_t t0 = 0; t0 < n_tiles; t0 += kPlanThreads) {
+  int64_t cost0 = 0;
+  for (int64_t t0 = 0; t0 < n_tiles[0]; t0 += kPlanThreads) {
     const int64_t t = t0 + tid;
-    int64_t units = 0, sum;
-    if (t < n_tiles) {
+    int64_t cost[1] = {0}, part[1];
+    if (t < n_tiles[0]) {
       const int q = last_at_most<int64_t>(pre, seqs, t);
-      const int64_t row0 = (t - pre[q]) * a.shape.rows, row1 = min(row0 + a.shape.rows, int64_t(r2_lo[q]) * G);
-      const int64_t p = r1_lo[q];
-      units = tile_span(v, int32_t(p + row0 / G), int32_t(p + (row1 - 1) / G), int32_t(p + r2_lo[q]), a.shape.unit_keys).n_units;
+      const int64_t first_row = (t - pre[q]) * a.shape.rows, row1 = min(first_row + a.shape.rows, int64_t(r2_lo[q]) * G);
+      const int32_t p = r1_lo[q];
+      cost[0] = a.overhead + tile_span(v, p + int32_t(first_row / G), p + int32_t((row1 - 1) / G), p + r2_lo[q],
+                                       a.shape.unit_keys).n_units;
     }
-    const int64_t end = units0 + block_scan(units, red, &sum);
-    if (t < n_tiles) v.unit_end[t] = end;
-    units0 += sum;
+    block_scan<1>(cost, red, part);
+    if (t < n_tiles[0]) v.cost_end[t] = cost0 + cost[0];
+    cost0 += part[0];
   }
   __syncthreads();
-  const int64_t all = units0 * v.kv_heads;
-  int groups = int(min(int64_t(a.max_groups), (all + a.min_units - 1) / a.min_units));
+  const int64_t all = cost0 * v.kv_heads;
+  const int groups = int(min(int64_t(a.max_groups), (all + a.min_cost - 1) / a.min_cost));
   if (tid <= groups) {
-    WorkStart w = {seqs, 0, int32_t(n_tiles), 0};
+    WorkStart w = {seqs, 0, int32_t(n_tiles[0]), 0};
     if (tid < groups) {
       const int64_t at = all * tid / groups;
-      // Sequence: the last one whose units begin at or before `at` and that has units.
+      // Sequence: the last one whose tiles begin at or before `at` (and that has tiles).
+      auto begin = [&](int q) { return pre[q] > 0 ? v.cost_end[pre[q] - 1] : int64_t(0); };
       int lo = 0, hi = seqs;
-      auto begin = [&](int q) { return pre[q] > 0 ? v.unit_end[pre[q] - 1] : int64_t(0); };
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (begin(mid) * v.kv_heads <= at) lo = mid;
@@ -390,19 +435,40 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
       const int64_t base = begin(lo), per_head = begin(lo + 1) - base, local = at - base * v.kv_heads;
       w.seq = lo;
       w.head = int32_t(local / per_head);
-      const int64_t x = base + local % per_head;  // unit of the sequence's tiles
-      int64_t t = pre[lo], e = pre[lo + 1];       // first tile whose units end behind x
+      const int64_t x = base + local % per_head;  // on the line of the sequence's tiles
+      int64_t t = pre[lo], e = pre[lo + 1];       // first tile that ends behind x
       while (t < e) {
         const int64_t mid = (t + e) >> 1;
-        if (v.unit_end[mid] > x) e = mid;
+        if (v.cost_end[mid] > x) e = mid;
         else t = mid + 1;
       }
       w.tile = int32_t(t);
-      w.unit = int32_t(x - (t > 0 ? v.unit_end[t - 1] : 0));
+      w.unit = int32_t(max(int64_t(0), x - (t > 0 ? v.cost_end[t - 1] : 0) - a.overhead));
     }
     v.starts[tid] = w;
+    starts[tid] = w;
   }
   if (tid == 0) v.header->groups = groups;
+  __syncthreads();
+  // Workgroup g is the first that begins inside its tile: the tile has parts from g - 1 on.
+  if (tid < groups) {
+    const WorkStart w = starts[tid];
+    int parts = 0;
+    if (w.unit > 0 && (starts[tid - 1].unit == 0 || starts[tid - 1].tile != w.tile || starts[tid - 1].head != w.head)) {
+      parts = 2;
+      for (int i = tid + 1; i < groups && starts[i].unit > 0 && starts[i].tile == w.tile && starts[i].head == w.head; ++i)
+        ++parts;
+    }
+    v.joins[tid] = parts;
+  }
+
+  if (a.fill) {
+    for (int64_t i = tid; i < a.rows; i += kPlanThreads) {
+      const int q = last_at_most<int32_t>(row_start, seqs, int32_t(i));
+      const int32_t o = int32_t(i) - row_start[q];
+      write_row(v, i, i < row_last && o < r2_lo[q], q, r1_lo[q] + o);
+    }
+  }
 }
 
 // Slot and position of every row of the step.
@@ -413,24 +479,9 @@ __global__ __launch_bounds__(kFillThreads) void paged_rows_kernel(PagedView v, i
   __syncthreads();
   const int64_t i = int64_t(blockIdx.x) * kFillThreads + threadIdx.x;
   if (i >= rows) return;
-  int64_t slot = -1;
-  int32_t t = 0, y = 0, x = 0;
-  if (i < start[v.seqs]) {
-    const int s = last_at_most<int32_t>(start, v.seqs, int32_t(i));
-    const int32_t o = int32_t(i) - start[s];
-    if (o < v.added[s]) {
-      const int32_t p = v.first[s] + o, frame = v.grid_h * v.grid_w;
-      const int32_t page = p / v.page_tokens;
-      slot = int64_t(v.table[size_t(s) * v.width + page]) * v.page_tokens + (p - page * v.page_tokens);
-      t = p / frame;
-      y = (p - t * frame) / v.grid_w;
-      x = p - t * frame - y * v.grid_w;
-    }
-  }
-  v.slots[i] = slot;
-  v.pos[3 * i] = t;
-  v.pos[3 * i + 1] = y;
-  v.pos[3 * i + 2] = x;
+  const int s = last_at_most<int32_t>(start, v.seqs, int32_t(i));
+  const int32_t o = int32_t(i) - start[s];
+  write_row(v, i, i < start[v.seqs] && o < v.added[s], s, v.first[s] + o);
 }
 
 struct PagedInsertArgs {
@@ -573,10 +624,12 @@ int fademem_paged_plan(fademem_paged* c, const int32_t* kept, const int32_t* add
   a.rows = rows;
   a.max_new = max_new;
   a.shape = step_shape(c);
-  a.max_groups = kPagedMaxGroups;
-  a.min_units = narrow_step(c) ? 1 : 4;
+  a.max_groups = a.shape.groups;
+  a.min_cost = a.shape.overhead + (narrow_step(c) ? 1 : 4);
+  a.overhead = a.shape.overhead;
+  a.fill = rows <= kFillInPlan;
   hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, as_stream(stream), a);
-  if (rows > 0)
+  if (!a.fill)
     hipLaunchKernelGGL(paged_rows_kernel, dim3(unsigned((rows + kFillThreads - 1) / kFillThreads)), dim3(kFillThreads), 0,
                        as_stream(stream), c->view, rows);
   const int rc = finish(c, stream);

@@ -112,25 +112,22 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, 
   if (a.lse && lane == 0) a.lse[size_t(qr.head) * a.rows + qr.row] = (m + log2f(l)) * kLn2;
 }
 
-constexpr int kJoinRows = 8;  // rows of a tile that one block joins
-
-// grid = (groups at most, row chunks of a tile).
+// grid = (groups at most, chunks of a tile's rows); a block joins kJoinRows rows,
+// a thread four elements of kPer of them, all its loads of two parts in flight.
+constexpr int kJoinRows = 32;
 template <bool BF16, int D>
 __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAttendArgs a, TileShape shape) {
   __shared__ float q_s[kFinishWaves][D];
   __shared__ int list[kFinishThreads], n_list;
   const PagedView& v = a.v;
   const int tid = threadIdx.x, wave = tid >> 6, g = blockIdx.x;
-  const int groups = v.header->groups;
+  const int groups = plan_array(&v.header->groups)[0];
+  const int parts = g > 0 && g < groups ? plan_array(v.joins)[g] : 0;
 
-  // Join the tile that boundary g is the first to cut.
-  const WorkStart w = g > 0 && g < groups ? v.starts[g] : WorkStart{0, 0, 0, 0};
-  bool first_cut = w.unit > 0;
-  if (first_cut) {
-    const WorkStart b = v.starts[g - 1];
-    first_cut = b.unit == 0 || b.tile != w.tile || b.head != w.head;
-  }
-  if (first_cut) {
+  // Join the tile that workgroup g is the first to begin inside: group g - 1's last
+  // units, then the first units of groups g, g + 1, ...
+  if (parts > 0) {
+    const WorkStart w = v.starts[g];
     Segment s;
     s.seq = w.seq;
     s.head = w.head;
@@ -139,48 +136,73 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
     s.q_start = v.q_start[w.seq];
     s.row0 = (w.tile - v.tile0[w.seq]) * shape.rows;
     s.rows = min(shape.rows, v.added[w.seq] * v.group - s.row0);
-    constexpr int kLanes = D / 4;  // threads of a row
-    const int r = blockIdx.y * kJoinRows + tid / kLanes, c = 4 * (tid % kLanes);
+    constexpr int kLanes = D / 4, kStep = kFinishThreads / kLanes, kPer = kJoinRows / kStep;
+    const int c = 4 * (tid % kLanes), r0 = blockIdx.y * kJoinRows + tid / kLanes;
+    const size_t slot = paged_slot_floats(shape.rows, D);
+    auto part = [&](int p) { return v.scratch + size_t(p == 0 ? 2 * g - 1 : 2 * (g + p - 1)) * slot; };
     bool bad = false;
-    if (tid < kJoinRows * kLanes && r < s.rows) {
-      // Parts: group g - 1's last units, then the first units of groups g, g+1, ... while they begin in this tile.
-      int parts = 2;
-      while (g + parts - 1 < groups) {
-        const WorkStart x = v.starts[g + parts - 1];
-        if (x.unit == 0 || x.tile != w.tile || x.head != w.head) break;
-        ++parts;
-      }
-      const size_t slot = paged_slot_floats(shape.rows, D);
-      auto part = [&](int p) { return v.scratch + size_t(p == 0 ? 2 * (g - 1) + 1 : 2 * (g + p - 1)) * slot; };
-      const size_t mi = size_t(shape.rows) * D + r, li = mi + shape.rows;
-      float m = -INFINITY;
-#pragma unroll 8
-      for (int p = 0; p < parts; ++p) m = fmaxf(m, part(p)[mi]);
-      const float ref = m == -INFINITY ? 0.0f : m;
-      float l = 0.0f, o[4] = {};
-#pragma unroll 8
-      for (int p = 0; p < parts; ++p) {
-        const float* x = part(p);
-        const float f = exp2f(x[mi] - ref);
-        const float4 y = *reinterpret_cast<const float4*>(x + size_t(r) * D + c);
-        l += f * x[li];
-        o[0] += f * y.x;
-        o[1] += f * y.y;
-        o[2] += f * y.z;
-        o[3] += f * y.w;
-      }
+    auto store = [&](int r, float m, float l, const float4& o) {
       const QueryRow q = query_row(v, s, r);
       const float inv = 1.0f / l;
       char* out = a.out + size_t(q.row) * a.out_pitch + (size_t(q.head) * D + c) * (BF16 ? 2 : 4);
       if constexpr (BF16) {
-        uint2 y = {round_pair(o[0] * inv, o[1] * inv), round_pair(o[2] * inv, o[3] * inv)};
+        const uint2 y = {round_pair(o.x * inv, o.y * inv), round_pair(o.z * inv, o.w * inv)};
         *reinterpret_cast<uint2*>(out) = y;
       } else {
-        *reinterpret_cast<float4*>(out) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+        *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
       }
       if (a.lse && c == 0) a.lse[size_t(q.head) * a.rows + q.row] = (m + log2f(l)) * kLn2;
-      const float sum = (o[0] + o[1]) + (o[2] + o[3]) + inv;
-      bad = !(fabsf(sum) < INFINITY);
+      const float sum = (o.x + o.y) + (o.z + o.w) + inv;
+      bad = bad || !(__builtin_fabsf(sum) < INFINITY);
+    };
+    if (parts == 2) {
+      const float *x = part(0), *y = part(1);
+      float4 ox[kPer], oy[kPer];
+      float mx[kPer], my[kPer], lx[kPer], ly[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int r = min(r0 + i * kStep, s.rows - 1);
+        ox[i] = *reinterpret_cast<const float4*>(x + size_t(r) * D + c);
+        oy[i] = *reinterpret_cast<const float4*>(y + size_t(r) * D + c);
+        mx[i] = x[shape.rows * D + r];
+        my[i] = y[shape.rows * D + r];
+        lx[i] = x[shape.rows * (D + 1) + r];
+        ly[i] = y[shape.rows * (D + 1) + r];
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int r = r0 + i * kStep;
+        if (r >= s.rows) break;
+        const float m = fmaxf(mx[i], my[i]), ref = m == -INFINITY ? 0.0f : m;
+        const float f = exp2f(mx[i] - ref), h = exp2f(my[i] - ref);
+        store(r, m, f * lx[i] + h * ly[i],
+              make_float4(f * ox[i].x + h * oy[i].x, f * ox[i].y + h * oy[i].y, f * ox[i].z + h * oy[i].z,
+                          f * ox[i].w + h * oy[i].w));
+      }
+    } else {
+      for (int i = 0; i < kPer; ++i) {
+        const int r = r0 + i * kStep;
+        if (r >= s.rows) break;
+        const int mi = shape.rows * D + r, li = mi + shape.rows;
+        float m = -INFINITY;
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) m = fmaxf(m, part(p)[mi]);
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float l = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) {
+          const float* x = part(p);
+          const float f = exp2f(x[mi] - ref);
+          const float4 y = *reinterpret_cast<const float4*>(x + size_t(r) * D + c);
+          l += f * x[li];
+          o.x += f * y.x;
+          o.y += f * y.y;
+          o.z += f * y.z;
+          o.w += f * y.w;
+        }
+        store(r, m, l, o);
+      }
     }
     if (__syncthreads_or(bad))
       for (int i = wave; i < kJoinRows; i += kFinishWaves)
@@ -242,7 +264,7 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
 hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, hipStream_t stream) {
   auto kernel = a.v.head_dim == 128 ? (bf16 ? paged_finish_kernel<true, 128> : paged_finish_kernel<false, 128>)
                                     : (bf16 ? paged_finish_kernel<true, 64> : paged_finish_kernel<false, 64>);
-  hipLaunchKernelGGL(kernel, dim3(kPagedMaxGroups, unsigned(shape.rows / kJoinRows)), dim3(kFinishThreads), 0, stream, a,
+  hipLaunchKernelGGL(kernel, dim3(unsigned(shape.groups), unsigned(shape.rows / kJoinRows)), dim3(kFinishThreads), 0, stream, a,
                      shape);
   return hipGetLastError();
 }

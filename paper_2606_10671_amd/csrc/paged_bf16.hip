@@ -75,14 +75,18 @@ __device__ __forceinline__ bf16x8 read_v(const char* buf, const ReadOffsets<D>& 
 
 // ---------------------------------------------------------------------------
 // Narrow tiles: 32 rows.  Bound by reading K and V once (a tile of 32 keys is
-// 16 KB and 16 MFMAs at D = 128).  The waves share out the keys, 32 of a unit of
-// 256 each, and stream them through LDS buffers of their own without barriers:
+// 16 KB and 16 MFMAs at D = 128).  Four waves share out the keys, 32 of a unit of
+// 128 each, and stream them through LDS buffers of their own without barriers:
 // K(t+1) is on its way while the scores of t are worked out, V(t+1) from P V(t)
-// on, so that half a workgroup's 128 KB are in flight at any time.  At the end
-// the waves' results are joined through LDS.
+// on, so that half a workgroup's 64 KB are in flight at any time.  Two workgroups
+// share a CU, so that one streams while the other begins or ends a tile.  At the
+// end the waves' results are joined through LDS.
 // ---------------------------------------------------------------------------
 
 constexpr int kNarrowKeys = 32;
+constexpr int kNarrowThreads = 256;
+constexpr int kNarrowWaves = kNarrowThreads / 64;
+static_assert(kPagedNarrowBf16.unit_keys == kNarrowWaves * kNarrowKeys, "a tile per wave");
 
 template <int D>
 __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
@@ -90,10 +94,10 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
   constexpr int kBuf = kNarrowKeys * D * 2;        // bytes of a wave's K (or V) buffer
   constexpr int kLoads = kBuf / 1024;              // 16-byte loads per lane
   constexpr int kO = 32 * D;                       // floats of a wave's O
-  static_assert(4 * kO * 4 == kWaves * kBuf, "four waves' O fit the K buffers, four the V buffers");
-  __shared__ __attribute__((aligned(16))) char k_lds[kWaves * kBuf];
-  __shared__ __attribute__((aligned(16))) char v_lds[kWaves * kBuf];
-  __shared__ float m_s[kWaves][32], l_s[kWaves][32];
+  static_assert(2 * kO * 4 == kNarrowWaves * kBuf, "two waves' O fit the K buffers, two the V buffers");
+  __shared__ __attribute__((aligned(16))) char k_lds[kNarrowWaves * kBuf];
+  __shared__ __attribute__((aligned(16))) char v_lds[kNarrowWaves * kBuf];
+  __shared__ float m_s[kNarrowWaves][32], l_s[kNarrowWaves][32];
   const PagedView& v = a.v;
   const int groups = plan_array(&v.header->groups)[0];
   if (int(blockIdx.x) >= groups) return;
@@ -131,7 +135,7 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
     auto keys_of = [&](int u) {
       Keys k;
       const bool sink = u < s.span.n_sink;
-      k.key0 = (sink ? u * 256 : s.span.from + (u - s.span.n_sink) * 256) + wave * kNarrowKeys;
+      k.key0 = (sink ? u * 128 : s.span.from + (u - s.span.n_sink) * 128) + wave * kNarrowKeys;
       k.lim = sink ? s.span.sinks : s.span.end;
       return k;
     };
@@ -236,10 +240,10 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
       }
     }
 
-    // Join the waves: O row by row in the tile buffers, waves 0-3 in K's, 4-7 in V's.
+    // Join the waves: O row by row in the tile buffers, waves 0-1 in K's, 2-3 in V's.
     l = pair_sum(l);
     __syncthreads();
-    float* mine = reinterpret_cast<float*>(wave < 4 ? k_lds : v_lds) + (wave & 3) * kO + l32 * D + 4 * hh;
+    float* mine = reinterpret_cast<float*>(wave < 2 ? k_lds : v_lds) + (wave & 1) * kO + l32 * D + 4 * hh;
     if (l32 < s.rows) {
 #pragma unroll
       for (int db = 0; db < R::DB; ++db)
@@ -257,18 +261,18 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
     bool bad = false;
     float* slot = v.scratch + size_t(s.slot(g)) * paged_slot_floats(32, D);
     constexpr int kLanes = D / 4;
-    for (int i = tid; i < s.rows * kLanes; i += kThreads) {
+    for (int i = tid; i < s.rows * kLanes; i += kNarrowThreads) {
       const int r = i / kLanes, c = 4 * (i % kLanes);
       float mm = m_s[0][r];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) mm = __builtin_elementwise_maximum(mm, m_s[w][r]);
+      for (int w = 1; w < kNarrowWaves; ++w) mm = __builtin_elementwise_maximum(mm, m_s[w][r]);
       const float ref = mm == -INFINITY ? 0.0f : mm;
       float ll = 0.0f, x[4] = {};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < kNarrowWaves; ++w) {
         const float f = __builtin_amdgcn_exp2f((m_s[w][r] - ref) * c2);
-        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(w < 4 ? k_lds : v_lds) +
-                                                          (w & 3) * kO + r * D + c);
+        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(w < 2 ? k_lds : v_lds) +
+                                                          (w & 1) * kO + r * D + c);
         ll += f * l_s[w][r];
         x[0] += f * y.x;
         x[1] += f * y.y;
@@ -695,7 +699,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 1) void paged_narrow_bf16(PagedAttendArgs a) {
+__global__ __launch_bounds__(kNarrowThreads, 2) void paged_narrow_bf16(PagedAttendArgs a) {
   paged_narrow_body<D>(a);
 }
 template <int D, bool WHOLE>
@@ -710,7 +714,8 @@ hipError_t launch_paged_bf16(const PagedAttendArgs& a, bool narrow, hipStream_t 
   auto kernel = narrow ? (d128 ? paged_narrow_bf16<128> : paged_narrow_bf16<64>)
                 : whole ? (d128 ? paged_wide_bf16<128, true> : paged_wide_bf16<64, true>)
                         : (d128 ? paged_wide_bf16<128, false> : paged_wide_bf16<64, false>);
-  hipLaunchKernelGGL(kernel, dim3(kPagedMaxGroups), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(narrow ? kPagedNarrowBf16.groups : kPagedWideBf16.groups)),
+                     dim3(narrow ? kNarrowThreads : kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -475,7 +475,8 @@ hipError_t launch_paged_f32(const PagedAttendArgs& a, bool narrow, hipStream_t s
   const bool d128 = a.v.head_dim == 128;
   auto kernel = narrow ? (d128 ? paged_narrow_f32<128> : paged_narrow_f32<64>)
                        : (d128 ? paged_wide_f32<128> : paged_wide_f32<64>);
-  hipLaunchKernelGGL(kernel, dim3(kPagedMaxGroups), dim3(narrow ? kNarrowThreads : kWideThreads), 0, stream, a);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(narrow ? kPagedNarrowF32.groups : kPagedWideF32.groups)),
+                     dim3(narrow ? kNarrowThreads : kWideThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -10,15 +10,15 @@
 namespace fademem {
 
 constexpr int kPagedMaxSeqs = 1024;   // one thread of the plan kernel per sequence
-constexpr int kPagedMaxGroups = 256;  // workgroups of one attention launch at most (one per CU)
+constexpr int kPagedMaxGroups = 512;  // workgroups of one attention launch at most
 
 // Attention work of a step.  The rows of a tile are (token, head of the group)
 // pairs of one sequence and one key head, token-major: row r is token r / G,
 // head r % G of the key head's G query heads, so that a tile of K and V serves
 // all of them.  A tile's keys come in units of `unit_keys`: first the units
 // that cover the sinks, then those that cover the window.  All units of a step
-// lie on one line, ordered by (sequence, key head, tile, unit), and are dealt
-// to the workgroups in equal runs: a run may end one tile's units, take some
+// lie on one line, ordered by (sequence, key head, tile, unit), each tile with its
+// overhead before it, and the line is dealt to the workgroups in equal runs: a run may end one tile's units, take some
 // tiles whole and begin another's.  Units of a tile that several workgroups
 // share leave partial results in their slots (0: a run's first units, which
 // continue a tile; 1: its last units, which begin one).
@@ -30,11 +30,13 @@ struct WorkStart {
 struct TileShape {
   int rows;       // query rows of a tile
   int unit_keys;  // keys of a unit
+  int groups;     // workgroups at most: those resident at once
+  int overhead;   // key units that a tile costs beside its own: first loads, last results
 };
-constexpr TileShape kPagedWideBf16 = {256, 64};
-constexpr TileShape kPagedNarrowBf16 = {32, 256};
-constexpr TileShape kPagedWideF32 = {128, 64};
-constexpr TileShape kPagedNarrowF32 = {32, 128};
+constexpr TileShape kPagedWideBf16 = {256, 64, 256, 4};
+constexpr TileShape kPagedNarrowBf16 = {32, 128, 512, 1};
+constexpr TileShape kPagedWideF32 = {128, 64, 256, 1};
+constexpr TileShape kPagedNarrowF32 = {32, 128, 256, 1};
 constexpr int kPagedMinTileRows = 32;
 
 // Floats of a partial result of a tile: O of every row, then row max and row sum.
@@ -62,8 +64,9 @@ struct PagedView {
   int64_t* slots;      // [max_rows]
   int32_t* pos;        // [max_rows][3]
   int32_t* tile0;      // [seqs + 1] first row tile of each sequence
-  int64_t* unit_end;   // [tiles] units of one head up to and with each tile
+  int64_t* cost_end;   // [tiles] cost of one head up to and with each tile, in key units
   WorkStart* starts;   // [groups + 1]
+  int32_t* joins;      // [groups]: parts of the tile that this workgroup is the first to begin inside, or 0
   uint64_t* redo;      // [tiles][kv_heads]: byte w != 0: rows 32 w.. of the tile have to be worked out again
   float* scratch;      // attention partials
   char* pages;         // layer 0

@@ -447,6 +447,24 @@ def current_stream() -> int:
     return int(raw(torch.cuda.current_device()))
 
 
+class _Here:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
+
+
+_HERE = _Here()
+
+
+def on_device(index: int):
+    """Context in which the device with this index is the current one (switching costs more than a small launch, so
+    only where another one is)."""
+    import torch
+    return _HERE if torch.cuda.current_device() == index else torch.cuda.device(index)
+
+
 class Cache:
     """Owns a device pool (a torch uint8 tensor) and a library handle.
 

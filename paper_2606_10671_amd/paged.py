@@ -56,6 +56,7 @@ class PagedCache:
             device = torch.device(device.type, torch.cuda.current_device())
         self.device = device
         self.rows = 0
+        self._seqs, self._heads, self._kv_heads, self._dim = int(seqs), int(heads), int(kv_heads), int(head_dim)
         with torch.cuda.device(device):
             self.pool = torch.empty(self.pool_bytes, dtype=torch.uint8, device=device)
             self.handle = fm.fademem_paged_create(self.cfg, self.pool.data_ptr(), self.pool_bytes, fm.current_stream())
@@ -83,21 +84,18 @@ class PagedCache:
         added[s] is."""
         import torch
         for name, t in (("kept", kept), ("added", added)):
-            if t.dtype != torch.int32 or tuple(t.shape) != (self.cfg.seqs,) or not t.is_contiguous() \
-                    or t.device != self.device:
-                raise ValueError(f"{name}: expected a contiguous int32 [{self.cfg.seqs}] tensor on {self.device}")
-        with torch.cuda.device(self.device):
+            if t.dtype != torch.int32 or t.shape != (self._seqs,) or not t.is_contiguous() or t.device != self.device:
+                raise ValueError(f"{name}: expected a contiguous int32 [{self._seqs}] tensor on {self.device}")
+        with fm.on_device(self.device.index):
             fm.fademem_paged_plan(self.handle, kept.data_ptr(), added.data_ptr(), rows, max_new, self._stream(stream))
         self.rows = rows
 
     def insert(self, k, v, layer: int = 0, rotary: Optional[Rotary] = None, stream=None):
         """The planned step's keys (turned by `rotary` to their positions) and
         values, [rows][kv_heads][head_dim], into the layer's pages."""
-        import torch
-        c = self.cfg
-        k_stride = rows_of(k, "k", self.torch_dtype, self.device, c.kv_heads, c.head_dim, self.rows)
-        v_stride = rows_of(v, "v", self.torch_dtype, self.device, c.kv_heads, c.head_dim, self.rows)
-        with torch.cuda.device(self.device):
+        k_stride = rows_of(k, "k", self.torch_dtype, self.device, self._kv_heads, self._dim, self.rows)
+        v_stride = rows_of(v, "v", self.torch_dtype, self.device, self._kv_heads, self._dim, self.rows)
+        with fm.on_device(self.device.index):
             fm.fademem_paged_insert(self.handle, layer, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
                                     None if rotary is None else rotary.rope, self._stream(stream))
 
@@ -106,15 +104,16 @@ class PagedCache:
         over the layer's pages.  Rows behind the last sequence's are left as
         they are in `out` and `lse` (float32 [heads][rows])."""
         import torch
-        c = self.cfg
-        q_stride = rows_of(q, "q", self.torch_dtype, self.device, c.heads, c.head_dim, self.rows)
+        rows, heads, dim = self.rows, self._heads, self._dim
+        q_stride = rows_of(q, "q", self.torch_dtype, self.device, heads, dim, rows)
         if out is None:
-            out = torch.empty((self.rows, c.heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
-        out_stride = rows_of(out, "out", self.torch_dtype, self.device, c.heads, c.head_dim, self.rows)
+            out, out_stride = torch.empty((rows, heads, dim), dtype=self.torch_dtype, device=self.device), heads * dim
+        else:
+            out_stride = rows_of(out, "out", self.torch_dtype, self.device, heads, dim, rows)
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != self.device
-                                or tuple(lse.shape) != (c.heads, self.rows)):
+                                or lse.shape != (heads, rows)):
             raise ValueError("lse: expected a contiguous float32 [heads][rows] tensor")
-        with torch.cuda.device(self.device):
+        with fm.on_device(self.device.index):
             fm.fademem_paged_attend(self.handle, layer, q.data_ptr(), q_stride, scale, out.data_ptr(), out_stride,
                                     0 if lse is None else lse.data_ptr(), self._stream(stream))
         return out

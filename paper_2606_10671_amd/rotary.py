@@ -10,22 +10,17 @@ from typing import Optional, Sequence
 from . import fademem as fm
 
 
-def rows_of(t, name: str, dtype, device, heads: Optional[int] = None, head_dim: Optional[int] = None,
-            rows: Optional[int] = None) -> int:
+def rows_of(t, name: str, dtype, device, heads: int, head_dim: int, rows: int) -> int:
     """Checks a [rows][heads][head_dim] tensor whose heads and elements are
     contiguous (rows may be apart) and returns its elements between rows."""
-    if t.dtype != dtype or not t.is_cuda or t.device != device or t.dim() != 3:
-        raise ValueError(f"{name}: expected a [rows][heads][head_dim] {dtype} tensor on {device}")
-    if (heads is not None and t.shape[1] != heads) or (head_dim is not None and t.shape[2] != head_dim):
-        raise ValueError(f"{name}: expected [rows][{heads}][{head_dim}]")
-    if rows is not None and t.shape[0] != rows:
-        raise ValueError(f"{name}: expected {rows} rows")
-    row = t.shape[1] * t.shape[2]
-    if t.numel() == 0:
-        return row
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+    if t.dtype != dtype or t.device != device or t.shape != (rows, heads, head_dim):
+        raise ValueError(f"{name}: expected a [{rows}][{heads}][{head_dim}] {dtype} tensor on {device}")
+    if t.is_contiguous():
+        return heads * head_dim
+    pitch, head, one = t.stride()
+    if (one != 1 and head_dim > 1) or (head != head_dim and heads > 1):
         raise ValueError(f"{name}: heads and elements must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else row
+    return pitch if rows > 1 else heads * head_dim
 
 
 class Rotary:
@@ -55,18 +50,19 @@ class Rotary:
         contiguous int32 [rows][3] tensor of (time, height, width).  out may be
         x.  inverse=True turns back: the gradient of apply."""
         import torch
-        if x.dtype not in (torch.float32, torch.bfloat16):
-            raise ValueError("x: expected float32 or bfloat16")
-        x_stride = rows_of(x, "x", x.dtype, x.device, head_dim=self.head_dim,
-                           heads=x.shape[1] if x.dim() == 3 else None)
-        rows, heads = x.shape[0], x.shape[1]
-        if pos.dtype != torch.int32 or tuple(pos.shape) != (rows, 3) or not pos.is_contiguous() or pos.device != x.device:
-            raise ValueError(f"pos: expected a contiguous int32 [{rows}][3] tensor on {x.device}")
+        dtype, device = x.dtype, x.device
+        if (dtype != torch.bfloat16 and dtype != torch.float32) or x.dim() != 3 or not x.is_cuda:
+            raise ValueError("x: expected a [rows][heads][head_dim] float32 or bfloat16 CUDA tensor")
+        rows, heads, _ = x.shape
+        x_stride = rows_of(x, "x", dtype, device, heads, self.head_dim, rows)
+        if pos.dtype != torch.int32 or pos.shape != (rows, 3) or not pos.is_contiguous() or pos.device != device:
+            raise ValueError(f"pos: expected a contiguous int32 [{rows}][3] tensor on {device}")
         if out is None:
-            out = torch.empty((rows, heads, self.head_dim), dtype=x.dtype, device=x.device)
-        y_stride = rows_of(out, "out", x.dtype, x.device, heads, self.head_dim, rows)
-        with torch.cuda.device(x.device):
-            fm.fademem_rope_apply(self.rope, fm.FADEMEM_BF16 if x.dtype == torch.bfloat16 else fm.FADEMEM_F32,
+            out, y_stride = torch.empty((rows, heads, self.head_dim), dtype=dtype, device=device), heads * self.head_dim
+        else:
+            y_stride = rows_of(out, "out", dtype, device, heads, self.head_dim, rows)
+        with fm.on_device(device.index):
+            fm.fademem_rope_apply(self.rope, fm.FADEMEM_BF16 if dtype == torch.bfloat16 else fm.FADEMEM_F32,
                                   pos.data_ptr(), rows, heads, x.data_ptr(), x_stride, out.data_ptr(), y_stride,
-                                  int(inverse), fm.current_stream() if stream is None else int(stream.cuda_stream))
+                                  1 if inverse else 0, fm.current_stream() if stream is None else int(stream.cuda_stream))
         return out

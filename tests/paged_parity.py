@@ -142,7 +142,8 @@ class Pair:
             assert np.isfinite(got).all(), where
         ok = np.isfinite(O)
         assert np.array_equal(np.isfinite(got), ok), (where, "finite")
-        err = np.abs(got - O)
+        with np.errstate(invalid="ignore"):
+            err = np.abs(got - O)
         assert (err[ok] <= tol[ok]).all(), (where, float((err - tol)[ok].max()), float(err[ok].max()))
         assert np.array_equal(np.isnan(got), np.isnan(O)) and (got[np.isinf(O)] == O[np.isinf(O)]).all(), where
         if got_l is not None:
