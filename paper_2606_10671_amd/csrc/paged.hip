@@ -94,6 +94,7 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   v->tile0 = reinterpret_cast<int32_t*>(take((seqs + 1) * 4));
   v->cost_end = reinterpret_cast<int64_t*>(take(uint64_t(max_tiles(c)) * 8));
   v->starts = reinterpret_cast<WorkStart*>(take((kPagedMaxGroups + 1) * sizeof(WorkStart)));
+  v->active = reinterpret_cast<int32_t*>(take(seqs * 4));
   v->joins = reinterpret_cast<int32_t*>(take(kPagedMaxGroups * sizeof(int32_t)));
   v->redo = reinterpret_cast<uint64_t*>(take((unsigned __int128)uint64_t(max_tiles(c)) * unsigned(c.kv_heads) * 8));
   const size_t wide_slots = 2 * size_t(wide.groups) * paged_slot_floats(wide.rows, c.head_dim);
@@ -170,37 +171,55 @@ constexpr int kPlanThreads = 1024;
 constexpr int64_t kFillInPlan = 4 * kPlanThreads;  // rows up to which the plan's block fills them itself
 constexpr int kPlanWaves = kPlanThreads / 64;
 
-// Inclusive prefix sums of N values over the block, in place; total[] gets the
-// sums.  red: N * kPlanWaves values of LDS.
-template <int N>
-__device__ __forceinline__ void block_scan(int64_t (&x)[N], int64_t* red, int64_t (&total)[N]) {
+// Inclusive prefix sum of a value below 2^25 over the wave: four shifts within rows
+// of 16 lanes, then the rows' last lanes broadcast to the rows behind them.  On
+// the vector ALU; through LDS permutes a scan of the block took 1.9 us.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
+// The same over the block, with the total.  red: kPlanWaves values of LDS that the
+// next call of this function does not use (calls alternate between two).
+struct Scan {
+  int64_t x, sum;
+};
+__device__ __forceinline__ Scan block_scan(uint32_t x, uint32_t* red) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    int64_t y[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) y[i] = __shfl_up(x[i], o);
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] += lane >= o ? y[i] : 0;
-  }
-  __syncthreads();  // the last call's sums have been read
-  if (lane == 63) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) red[i * kPlanWaves + wave] = x[i];
-  }
+  x = wave_scan(x);
+  if (lane == 63) red[wave] = x;  // below 2^31
   __syncthreads();
+  int64_t before = 0, sum = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    int64_t before = 0, sum = 0;
+  for (int w = 0; w < kPlanWaves; w += 4) {
+    const uint4 y = *reinterpret_cast<const uint4*>(red + w);
+    const uint32_t v[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int w = 0; w < kPlanWaves; ++w) {
-      const int64_t y = red[i * kPlanWaves + w];
-      before += w < wave ? y : 0;
-      sum += y;
+    for (int i = 0; i < 4; ++i) {
+      before += w + i < wave ? v[i] : 0u;
+      sum += v[i];
     }
-    x[i] += before;
-    total[i] = sum;
   }
+  return {before + int64_t(x), sum};
+}
+
+// Position of the k-th (from 0) set bit.
+__device__ __forceinline__ int nth_bit(uint32_t bits, int k) {
+  int at = 0;
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) {
+    const int c = __popc((bits >> at) & ((1u << w) - 1u));
+    if (k >= c) {
+      k -= c;
+      at += w;
+    }
+  }
+  return at;
 }
 
 // Last i in [0, n) with a[i] <= x (a[0] <= x, a not decreasing).
@@ -215,15 +234,14 @@ __device__ __forceinline__ int last_at_most(const T* a, int n, T x) {
   return lo;
 }
 
+constexpr int kCostsInLds = 4096;  // tiles whose costs the search for the workgroups' starts finds in LDS
+
 struct PlanArgs {
   PagedView v;
   const int32_t* kept;
   const int32_t* added;
   int64_t rows, max_new;
   TileShape shape;
-  int max_groups;
-  int min_cost;   // key units (a tile's overhead among them) of a workgroup at least
-  int overhead;   // key units that a tile costs beside its own
   int fill;       // 1: this kernel also writes the rows' slots and positions
 };
 
@@ -232,7 +250,7 @@ __device__ __forceinline__ void write_row(const PagedView& v, int64_t i, bool li
   int64_t slot = -1;
   int32_t t = 0, y = 0, x = 0;
   if (live) {
-    const int32_t frame = v.grid_h * v.grid_w, page = p / v.page_tokens;
+    const int32_t frame = v.grid_h * v.grid_w, page = page_of(v, p);
     slot = int64_t(v.table[size_t(s) * v.width + page]) * v.page_tokens + (p - page * v.page_tokens);
     t = p / frame;
     y = (p - t * frame) / v.grid_w;
@@ -244,6 +262,37 @@ __device__ __forceinline__ void write_row(const PagedView& v, int64_t i, bool li
   v.pos[3 * i + 2] = x;
 }
 
+// The even dealing of `total` tiles of `units` key units (EvenPlan); returns the
+// workgroups with work.  Head parts: as many as the groups allow, none shorter
+// than the shape's least.  Tails for the groups left over: a tail costs its
+// group the overhead of a tile again, counted as half of shape.overhead beyond a
+// head part's own; tails that take less than two units off every head part are
+// left out.
+constexpr int kMinTailSaves = 2;
+__device__ int even_plan(int total, int units, int tiles, TileShape shape, EvenPlan* e) {
+  e->even = 1;
+  e->groups = shape.groups;
+  e->units = units;
+  e->tiles = tiles;
+  e->rounds = total / shape.groups;
+  e->rem = total - e->rounds * shape.groups;
+  e->heads = e->tails_per = 1;
+  e->tail_len = 0;
+  if (e->rem > 0) {
+    e->heads = max(1, min(shape.groups / e->rem, units / shape.min_part));
+    const int left = shape.groups - e->heads * e->rem;
+    if (left > 0 && units >= shape.min_part) {
+      e->tails_per = (e->rem + left - 1) / left;
+      const int over = (shape.overhead + 1) / 2 * (e->tails_per - 1) * e->heads;
+      const int len = units > over ? (units - over) / (e->tails_per * e->heads + 1) : 0;
+      if (len >= kMinTailSaves * e->heads) e->tail_len = len;
+    }
+  }
+  e->head_len = units - e->tail_len;
+  if (e->rounds > 0) return shape.groups;
+  return e->heads * e->rem + (e->tail_len > 0 ? (e->rem + e->tails_per - 1) / e->tails_per : 0);
+}
+
 // The step's plan, one block: thread s has sequence s.  What each sequence gives
 // back and needs follows from its lengths alone; prefix sums over the sequences
 // say where its rows, pages and row tiles begin.  Pages are bits of a map, so
@@ -252,11 +301,14 @@ __device__ __forceinline__ void write_row(const PagedView& v, int64_t i, bool li
 // prefix sums over the row tiles -> the workgroups' starts.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   const PagedView& v = a.v;
-  __shared__ int64_t red[2 * kPlanWaves];
+  __shared__ __attribute__((aligned(16))) uint32_t red_a[kPlanWaves], red_b[kPlanWaves];
+  __shared__ uint32_t word_s[kPlanThreads], word_pre[kPlanThreads];
   __shared__ int64_t pre[kPagedMaxSeqs + 1];  // prefix sums of what the phase deals out
   __shared__ int32_t r1_lo[kPagedMaxSeqs], r1_n[kPagedMaxSeqs], r2_lo[kPagedMaxSeqs];
   __shared__ int32_t row_start[kPagedMaxSeqs + 1];
   __shared__ WorkStart starts[kPagedMaxGroups + 1];
+  __shared__ int64_t cost_s[kCostsInLds], base_s[kPagedMaxSeqs + 1];
+  __shared__ int32_t even_tiles, even_units;  // of the first sequence with tiles, of the first tile
   const int tid = threadIdx.x, s = tid, seqs = v.seqs;
   const bool live = s < seqs;
   const int64_t P = v.page_tokens;
@@ -266,23 +318,24 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   const int64_t k = live ? a.kept[s] : 0, n = live ? a.added[s] : 0, held = live ? v.held[s] : 0;
   const int32_t gone = live ? v.gone[s] : 0;
   const int64_t want_rows = live && n > 0 ? n : 0;
-  int64_t row_end[1] = {want_rows}, row_total[1];
-  block_scan<1>(row_end, red, row_total);
+  const Scan rows = block_scan(uint32_t(min(want_rows, a.rows + 1)), red_a);
   int32_t code = FADEMEM_OK;
-  if (k < 0 || n < 0 || n > a.max_new || k > held || k + n > v.max_tokens || (n > 0 && row_end[0] > a.rows))
+  if (k < 0 || n < 0 || n > a.max_new || k > held || k + n > v.max_tokens || (n > 0 && rows.x > a.rows))
     code = FADEMEM_EINVAL;
   const int32_t front = v.front;
-  const int64_t low_page = code ? 0 : paged_low(v, int32_t(k)) / P;
+  const int32_t k32 = code ? 0 : int32_t(k), n32 = code ? 0 : int32_t(n);
+  const int32_t low_page = page_of(v, paged_low(v, k32));
   const bool restart = gone > front && k <= front * P;  // all that is kept lies in the sinks' pages
   if (!code && gone > front && !restart && low_page < gone) code = FADEMEM_ESTATE;
   const bool ok = live && code == FADEMEM_OK;
 
   // Pages that go (two ranges) and pages needed, for `m` new tokens.
-  const int32_t top = int32_t(low_page > front ? low_page : front);
-  const int32_t np_old = int32_t((held + P - 1) / P);
+  const int32_t top = max(low_page, front);
+  auto pages_of = [&](int32_t tokens) { return tokens > 0 ? page_of(v, tokens - 1) + 1 : 0; };
+  const int32_t np_old = pages_of(int32_t(held));
   int32_t lo1 = 0, n1 = 0, lo2 = 0, n2 = 0, need = 0, from = 0;
-  auto pages_for = [&](int64_t m) {
-    const int32_t np = int32_t((k + m + P - 1) / P);
+  auto pages_for = [&](int32_t m) {
+    const int32_t np = pages_of(k32 + m);
     n1 = n2 = need = 0;
     if (!ok) return;
     if (restart) {
@@ -298,27 +351,25 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
       n2 = max(0, np_old - np);
       from = np_old;
     }
-    need = max(0, np - from);
+    need = min(max(0, np - from), int32_t(v.n_pages) + 1);  // more never fit
   };
-  pages_for(n);
-  int64_t end[2] = {int64_t(n1) + n2, need}, sum[2];
-  block_scan<2>(end, red, sum);
-  if (sum[1] > free0 + sum[0]) {  // not all fit: the sequences behind the first that does not stay as they are
-    if (ok && need > 0 && end[1] > free0 + sum[0]) {
+  pages_for(n32);
+  Scan going = block_scan(uint32_t(n1 + n2), red_b), taken = block_scan(uint32_t(need), red_a);
+  if (taken.sum > free0 + going.sum) {  // not all fit: the sequences from the first that does not on take none
+    if (ok && need > 0 && taken.x > free0 + going.sum) {
       code = FADEMEM_ENOMEM;
       pages_for(0);
     }
-    end[0] = int64_t(n1) + n2;
-    end[1] = need;
-    block_scan<2>(end, red, sum);
+    going = block_scan(uint32_t(n1 + n2), red_b);
+    taken = block_scan(uint32_t(need), red_a);
   }
   const bool admitted = ok && code == FADEMEM_OK;
-  const int64_t released = sum[0], given = sum[1];
+  const int64_t released = going.sum, given = taken.sum;
 
   // Release.
   if (released > 0) {
     if (live) {
-      pre[s] = end[0] - n1 - n2;
+      pre[s] = going.x - n1 - n2;
       r1_lo[s] = lo1;
       r1_n[s] = n1;
       r2_lo[s] = lo2;
@@ -339,36 +390,40 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   // Allocation: the i-th lowest free page is the i-th needed one.
   if (given > 0) {
     if (live) {
-      pre[s] = end[1] - need;
+      pre[s] = taken.x - need;
       r1_lo[s] = from;
     }
     __syncthreads();
     const int64_t words = (v.n_pages + 31) / 32;
-    int64_t rank0 = 0;
-    for (int64_t w0 = 0; w0 < words && rank0 < given; w0 += kPlanThreads) {
+    int64_t done = 0;
+    for (int64_t w0 = 0; w0 < words && done < given; w0 += kPlanThreads) {
       const int64_t w = w0 + tid;
-      uint32_t bits = w < words ? __hip_atomic_load(v.bitmap + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+      const uint32_t bits = w < words ? __hip_atomic_load(v.bitmap + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
       const int cnt = __popc(bits);
-      int64_t upto[1] = {cnt}, found[1];
-      block_scan<1>(upto, red, found);
-      int64_t rank = rank0 + upto[0] - cnt;
-      const uint32_t before = bits;
-      while (bits && rank < given) {
-        const int b = __ffs(bits) - 1;
-        bits &= bits - 1;
-        const int q = last_at_most<int64_t>(pre, seqs, rank);
-        v.table[size_t(q) * v.width + r1_lo[q] + int32_t(rank - pre[q])] = int32_t(w * 32 + b);
-        ++rank;
+      const Scan upto = block_scan(cnt, red_b);
+      const int64_t first = upto.x - cnt;  // rank of the word's first free page in this round
+      word_s[tid] = bits;
+      word_pre[tid] = uint32_t(first);
+      const int64_t take = min(upto.sum, given - done);  // of this round
+      const int m = int(max(int64_t(0), min(int64_t(cnt), take - first)));
+      if (m > 0)
+        __hip_atomic_store(v.bitmap + w, m == cnt ? 0u : bits & (0xffffffffu << nth_bit(bits, m)), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      for (int64_t r = tid; r < take; r += kPlanThreads) {
+        const int i = last_at_most<uint32_t>(word_pre, kPlanThreads, uint32_t(r));
+        const int q = last_at_most<int64_t>(pre, seqs, done + r);
+        v.table[size_t(q) * v.width + r1_lo[q] + int32_t(done + r - pre[q])] =
+            int32_t((w0 + i) * 32 + nth_bit(word_s[i], int(r - word_pre[i])));
       }
-      if (bits != before) __hip_atomic_store(v.bitmap + w, bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      rank0 += found[0];
+      done += take;
+      __syncthreads();
     }
-    __syncthreads();
   }
 
   // State.
   const int64_t fresh = admitted ? n : 0;
-  const int32_t row0 = int32_t(min(row_end[0] - want_rows, a.rows)), row_last = int32_t(min(row_total[0], a.rows));
+  const int32_t row0 = int32_t(min(rows.x - min(want_rows, a.rows + 1), a.rows)), row_last = int32_t(min(rows.sum, a.rows));
   if (live) {
     v.status[s] = code;
     v.first[s] = int32_t(ok ? k : 0);
@@ -386,69 +441,99 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
 
   // The attention's work: row tiles, their costs in key units, where each workgroup starts.
   const int G = v.group;
-  const int tiles_s = int((fresh * G + a.shape.rows - 1) / a.shape.rows);
-  int64_t tile_end[1] = {tiles_s}, n_tiles[1];
-  block_scan<1>(tile_end, red, n_tiles);
+  const int tiles_s = (int(fresh) * G + a.shape.rows - 1) / a.shape.rows;
+  const Scan tiles = block_scan(tiles_s, red_b), live_seqs = block_scan(fresh > 0, red_a);
+  const int64_t n_tiles = tiles.sum;
   if (live) {
-    pre[s] = tile_end[0] - tiles_s;
-    v.tile0[s] = int32_t(tile_end[0] - tiles_s);
+    if (fresh > 0) {
+      v.active[live_seqs.x - 1] = s;
+      if (live_seqs.x == 1) even_tiles = tiles_s;
+    }
+    pre[s] = tiles.x - tiles_s;
+    v.tile0[s] = int32_t(tiles.x - tiles_s);
     r1_lo[s] = int32_t(k);
     r2_lo[s] = int32_t(fresh);
     row_start[s] = row0;
   }
   if (tid == 0) {
-    pre[seqs] = n_tiles[0];
-    v.tile0[seqs] = int32_t(n_tiles[0]);
+    pre[seqs] = n_tiles;
+    v.tile0[seqs] = int32_t(n_tiles);
     row_start[seqs] = row_last;
   }
   __syncthreads();
+  bool even = a.shape.even && (tiles_s == 0 || tiles_s == even_tiles);
+  const bool one_each = !a.shape.even;
   int64_t cost0 = 0;
-  for (int64_t t0 = 0; t0 < n_tiles[0]; t0 += kPlanThreads) {
-    const int64_t t = t0 + tid;
-    int64_t cost[1] = {0}, part[1];
-    if (t < n_tiles[0]) {
-      const int q = last_at_most<int64_t>(pre, seqs, t);
-      const int64_t first_row = (t - pre[q]) * a.shape.rows, row1 = min(first_row + a.shape.rows, int64_t(r2_lo[q]) * G);
+  for (int64_t t0 = 0; t0 < n_tiles; t0 += kPlanThreads) {
+    // Narrow tiles: one for every sequence with new tokens, worked out by the sequence's thread.
+    const int64_t t = one_each ? pre[min(s, seqs)] : t0 + tid;
+    const bool has = one_each ? tiles_s > 0 : t < n_tiles;
+    int64_t cost = 0;
+    if (has) {
+      const int q = one_each ? s : last_at_most<int64_t>(pre, seqs, t);
+      const int first_row = int(t - pre[q]) * a.shape.rows, row1 = min(first_row + a.shape.rows, r2_lo[q] * G);
       const int32_t p = r1_lo[q];
-      cost[0] = a.overhead + tile_span(v, p + int32_t(first_row / G), p + int32_t((row1 - 1) / G), p + r2_lo[q],
-                                       a.shape.unit_keys).n_units;
+      cost = a.shape.overhead + tile_span(v, p + first_row / G, p + (row1 - 1) / G, p + r2_lo[q], a.shape.unit_keys).n_units;
     }
-    block_scan<1>(cost, red, part);
-    if (t < n_tiles[0]) v.cost_end[t] = cost0 + cost[0];
-    cost0 += part[0];
+    const int32_t units = int32_t(cost) - a.shape.overhead;
+    if (t == 0) even_units = units;
+    const Scan upto = block_scan(uint32_t(cost), t0 / kPlanThreads % 2 ? red_a : red_b);
+    even = even && (!has || units == even_units);
+    if (has) {
+      v.cost_end[t] = cost0 + upto.x;
+      if (t < kCostsInLds) cost_s[t] = cost0 + upto.x;
+    }
+    cost0 += upto.sum;
   }
   __syncthreads();
+  even = __syncthreads_and(even) && n_tiles * v.kv_heads < (int64_t(1) << 30);
   const int64_t all = cost0 * v.kv_heads;
-  const int groups = int(min(int64_t(a.max_groups), (all + a.min_cost - 1) / a.min_cost));
-  if (tid <= groups) {
-    WorkStart w = {seqs, 0, int32_t(n_tiles[0]), 0};
+  const int min_cost = a.shape.overhead + a.shape.min_part;
+  int groups = all >= int64_t(a.shape.groups) * min_cost ? a.shape.groups : (int(all) + min_cost - 1) / min_cost;
+  auto cost_end = [&](int64_t t) { return t < kCostsInLds ? cost_s[t] : v.cost_end[t]; };
+  if (even) {
+    groups = 0;
+  } else {
+    if (s <= seqs) base_s[s] = pre[s] > 0 ? cost_end(pre[s] - 1) : 0;  // where each sequence's tiles begin
+    if (seqs == kPlanThreads && tid == 0) base_s[seqs] = cost0;
+    __syncthreads();
+  }
+  if (tid <= groups && groups > 0) {
+    WorkStart w = {seqs, 0, int32_t(n_tiles), 0};
     if (tid < groups) {
-      const int64_t at = all * tid / groups;
-      // Sequence: the last one whose tiles begin at or before `at` (and that has tiles).
-      auto begin = [&](int q) { return pre[q] > 0 ? v.cost_end[pre[q] - 1] : int64_t(0); };
+      const int64_t at = int64_t(double(all) * double(tid) / double(groups));  // rises with tid and stays below `all`
+      // The last sequence that begins at or before `at`: it has tiles.
       int lo = 0, hi = seqs;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (begin(mid) * v.kv_heads <= at) lo = mid;
+        if (base_s[mid] * v.kv_heads <= at) lo = mid;
         else hi = mid;
       }
-      const int64_t base = begin(lo), per_head = begin(lo + 1) - base, local = at - base * v.kv_heads;
       w.seq = lo;
-      w.head = int32_t(local / per_head);
-      const int64_t x = base + local % per_head;  // on the line of the sequence's tiles
-      int64_t t = pre[lo], e = pre[lo + 1];       // first tile that ends behind x
+      const int64_t base = base_s[lo], per_head = base_s[lo + 1] - base, local = at - base * v.kv_heads;
+      w.head = int32_t(double(local) / double(per_head));  // within one of the quotient; made exact
+      w.head += (w.head + 1) * per_head <= local ? 1 : 0;
+      w.head -= w.head * per_head > local ? 1 : 0;
+      const int64_t x = base + local - w.head * per_head;  // on the line of the sequence's tiles
+      int64_t t = pre[w.seq], e = pre[w.seq + 1];          // first tile that ends behind x
       while (t < e) {
         const int64_t mid = (t + e) >> 1;
-        if (v.cost_end[mid] > x) e = mid;
+        if (cost_end(mid) > x) e = mid;
         else t = mid + 1;
       }
       w.tile = int32_t(t);
-      w.unit = int32_t(max(int64_t(0), x - (t > 0 ? v.cost_end[t - 1] : 0) - a.overhead));
+      w.unit = int32_t(max(int64_t(0), x - (t > 0 ? cost_end(t - 1) : 0) - a.shape.overhead));
     }
     v.starts[tid] = w;
     starts[tid] = w;
   }
-  if (tid == 0) v.header->groups = groups;
+  if (tid == 0) {
+    EvenPlan e = {};
+    int launched = groups;
+    if (even && n_tiles > 0) launched = even_plan(int(n_tiles * v.kv_heads), even_units, even_tiles, a.shape, &e);
+    v.header->groups = launched;
+    v.header->even = e;
+  }
   __syncthreads();
   // Workgroup g is the first that begins inside its tile: the tile has parts from g - 1 on.
   if (tid < groups) {
@@ -624,9 +709,6 @@ int fademem_paged_plan(fademem_paged* c, const int32_t* kept, const int32_t* add
   a.rows = rows;
   a.max_new = max_new;
   a.shape = step_shape(c);
-  a.max_groups = a.shape.groups;
-  a.min_cost = a.shape.overhead + (narrow_step(c) ? 1 : 4);
-  a.overhead = a.shape.overhead;
   a.fill = rows <= kFillInPlan;
   hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, as_stream(stream), a);
   if (!a.fill)
@@ -692,10 +774,7 @@ int fademem_paged_insert(fademem_paged* c, int32_t layer, const void* k, int64_t
   a.kv_heads = c->cfg.kv_heads;
   a.head_dim = c->cfg.head_dim;
   a.page_tokens = c->cfg.page_tokens;
-  const int per_row = int(2 * row * elt / 16);
-  int64_t per = 1024 / per_row;
-  if (per > (a.rows + 511) / 512) per = (a.rows + 511) / 512;
-  a.per_block = int(per < 1 ? 1 : per > kRotMaxRows ? kRotMaxRows : per);
+  a.per_block = rows_per_block(a.rows, int(2 * row * elt / 16), a.rot.pairs);
   const bool bf16 = c->cfg.dtype == FADEMEM_BF16, halves = rope && a.rot.halves;
   auto kernel = bf16 ? (halves ? paged_insert_kernel<true, true> : paged_insert_kernel<true, false>)
                      : (halves ? paged_insert_kernel<false, true> : paged_insert_kernel<false, false>);

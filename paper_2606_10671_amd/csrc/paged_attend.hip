@@ -118,28 +118,39 @@ constexpr int kJoinRows = 32;
 template <bool BF16, int D>
 __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAttendArgs a, TileShape shape) {
   __shared__ float q_s[kFinishWaves][D];
-  __shared__ int list[kFinishThreads], n_list;
+  __shared__ int list[kFinishThreads + 1], n_list;
   const PagedView& v = a.v;
   const int tid = threadIdx.x, wave = tid >> 6, g = blockIdx.x;
-  const int groups = plan_array(&v.header->groups)[0];
-  const int parts = g > 0 && g < groups ? plan_array(v.joins)[g] : 0;
-
   // Join the tile that workgroup g is the first to begin inside: group g - 1's last
-  // units, then the first units of groups g, g + 1, ...
-  if (parts > 0) {
-    const WorkStart w = v.starts[g];
+  // units, then the first units of groups g, g + 1, ...; of an even plan, tile g of
+  // those left over.
+  const EvenPlan even = v.header->even;
+  const bool is_even = shape.even && even.even;
+  const int groups = plan_array(&v.header->groups)[0];
+  int parts = 0;
+  if (is_even) {
+    if (g < even.rem) parts = even.heads + (even.tail_len > 0 ? 1 : 0);
+  } else if (g > 0 && g < groups) {
+    parts = plan_array(v.joins)[g];
+  }
+  Segment mine = {};
+  bool again = false;
+  if (parts > 1) {
     Segment s;
-    s.seq = w.seq;
-    s.head = w.head;
-    s.first = v.first[w.seq];
-    s.held = v.held[w.seq];
-    s.q_start = v.q_start[w.seq];
-    s.row0 = (w.tile - v.tile0[w.seq]) * shape.rows;
-    s.rows = min(shape.rows, v.added[w.seq] * v.group - s.row0);
+    if (is_even) {
+      even_tile(v, shape, even.tiles, even.rounds * even.groups + g, s);
+    } else {
+      const WorkStart w = v.starts[g];
+      s.seq = w.seq;
+      s.head = w.head;
+      s.tile = w.tile;
+      describe(v, shape, v.tile0[w.seq], s);
+    }
+    const int slot0 = is_even ? g : 2 * g - 1, slot1 = is_even ? g + even.rem : 2 * g, step = is_even ? even.rem : 2;
     constexpr int kLanes = D / 4, kStep = kFinishThreads / kLanes, kPer = kJoinRows / kStep;
     const int c = 4 * (tid % kLanes), r0 = blockIdx.y * kJoinRows + tid / kLanes;
     const size_t slot = paged_slot_floats(shape.rows, D);
-    auto part = [&](int p) { return v.scratch + size_t(p == 0 ? 2 * g - 1 : 2 * (g + p - 1)) * slot; };
+    auto part = [&](int p) { return v.scratch + size_t(p == 0 ? slot0 : slot1 + (p - 1) * step) * slot; };
     bool bad = false;
     auto store = [&](int r, float m, float l, const float4& o) {
       const QueryRow q = query_row(v, s, r);
@@ -204,45 +215,50 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
         store(r, m, l, o);
       }
     }
-    if (__syncthreads_or(bad))
-      for (int i = wave; i < kJoinRows; i += kFinishWaves)
-        if (int(blockIdx.y) * kJoinRows + i < s.rows)
-          attend_row<BF16, D>(a, s.seq, query_row(v, s, blockIdx.y * kJoinRows + i), q_s[wave]);
+    again = __syncthreads_or(bad);
+    mine = s;
   }
-  if (blockIdx.y > 0) return;
 
-  // Rows of tiles that one workgroup finished, marked by it.
-  const int64_t jobs = int64_t(v.tile0[v.seqs]) * v.kv_heads;
-  for (int64_t j0 = int64_t(g) * kFinishThreads; j0 < jobs; j0 += int64_t(gridDim.x) * kFinishThreads) {
+  // Rows again: this block's, if joining them gave something that is not finite,
+  // and rows of whole tiles that the attention marked.
+  const int64_t jobs = blockIdx.y == 0 ? int64_t(v.tile0[v.seqs]) * v.kv_heads : 0;
+  for (int64_t j0 = int64_t(g) * kFinishThreads; again || j0 < jobs; j0 += int64_t(gridDim.x) * kFinishThreads) {
     const uint64_t mark = j0 + tid < jobs ? v.redo[j0 + tid] : 0;
-    if (!__syncthreads_or(mark != 0)) continue;
-    if (tid == 0) n_list = 0;
+    if (!__syncthreads_or(mark != 0) && !again) continue;
+    if (tid == 0) {
+      n_list = again;
+      list[0] = -1;
+    }
     __syncthreads();
     if (mark) list[atomicAdd(&n_list, 1)] = tid;
     __syncthreads();
     for (int i = 0; i < n_list; ++i) {
-      const int64_t j = j0 + list[i];
-      const uint64_t marks = v.redo[j];
-      const int tile = int(j / v.kv_heads);
-      int lo = 0, hi = v.seqs;  // the last sequence whose tiles begin at or before it
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (v.tile0[mid] <= tile) lo = mid;
-        else hi = mid;
+      Segment s = mine;
+      int r0 = blockIdx.y * kJoinRows, r1 = min(r0 + kJoinRows, mine.rows);
+      uint64_t marks = ~uint64_t(0);
+      if (list[i] >= 0) {
+        const int64_t j = j0 + list[i];
+        s.tile = int(j / v.kv_heads);
+        s.head = int(j - int64_t(s.tile) * v.kv_heads);
+        int lo = 0, hi = v.seqs;  // the last sequence whose tiles begin at or before it
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (v.tile0[mid] <= s.tile) lo = mid;
+          else hi = mid;
+        }
+        s.seq = lo;
+        describe(v, shape, v.tile0[lo], s);
+        r0 = 0;
+        r1 = s.rows;
+        marks = v.redo[j];
       }
-      Segment s;
-      s.seq = lo;
-      s.head = int(j - int64_t(tile) * v.kv_heads);
-      s.first = v.first[lo];
-      s.held = v.held[lo];
-      s.q_start = v.q_start[lo];
-      s.row0 = (tile - v.tile0[lo]) * shape.rows;
-      s.rows = min(shape.rows, v.added[lo] * v.group - s.row0);
-      for (int r = wave; r < s.rows; r += kFinishWaves)
-        if ((marks >> (8 * (r >> 5))) & 0xff) attend_row<BF16, D>(a, lo, query_row(v, s, r), q_s[wave]);
+      for (int r = r0 + wave; r < r1; r += kFinishWaves)
+        if ((marks >> (8 * (r >> 5))) & 0xff) attend_row<BF16, D>(a, s.seq, query_row(v, s, r), q_s[wave]);
     }
+    again = false;
     __syncthreads();
   }
+  if (blockIdx.y > 0) return;
 
   // Rows of sequences that were not admitted.
   for (int s = g; s < v.seqs; s += gridDim.x) {

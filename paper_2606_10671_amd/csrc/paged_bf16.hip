@@ -257,9 +257,9 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
       }
     }
     __syncthreads();
-    const bool whole = s.whole();
+    const bool whole = s.slot < 0;
     bool bad = false;
-    float* slot = v.scratch + size_t(s.slot(g)) * paged_slot_floats(32, D);
+    float* slot = v.scratch + size_t(max(s.slot, 0)) * paged_slot_floats(32, D);
     constexpr int kLanes = D / 4;
     for (int i = tid; i < s.rows * kLanes; i += kNarrowThreads) {
       const int r = i / kLanes, c = 4 * (i % kLanes);
@@ -659,7 +659,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
 
     l = pair_sum(l);
     const int r = wave * 32 + l32;
-    if (s.whole()) {
+    if (s.slot < 0) {
       const float inv = 1.0f / l;
       float all = inv;
       char* out = a.out + size_t(qr.row) * a.out_pitch + size_t(qr.head) * D * 2;
@@ -679,7 +679,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
       const bool bad = __any(r < s.rows && !(__builtin_fabsf(all) < INFINITY));
       if (lane == 0) reinterpret_cast<uint8_t*>(v.redo + size_t(s.tile) * v.kv_heads + s.head)[wave] = bad ? 1 : 0;
     } else {
-      float* slot = v.scratch + size_t(s.slot(g)) * paged_slot_floats(kPagedWideBf16.rows, D);
+      float* slot = v.scratch + size_t(max(s.slot, 0)) * paged_slot_floats(kPagedWideBf16.rows, D);
       if (r < s.rows) {
         float* row = slot + size_t(r) * D + 4 * hh;
 #pragma unroll

@@ -19,9 +19,6 @@ __device__ __forceinline__ const CONST_AS T* plan_array(const T* p) {
   return (const CONST_AS T*)p;
 }
 
-__device__ __forceinline__ int page_of(const PagedView& v, int key) {
-  return int((uint64_t(uint32_t(key)) * v.page_magic) >> v.page_shift);
-}
 __device__ __forceinline__ int32_t safe_page(const PagedView& v, int32_t id) {
   return min(max(id, 0), int32_t(v.n_pages) - 1);
 }
@@ -44,49 +41,94 @@ __device__ __forceinline__ void wait_lds() {
 struct Segment {
   int seq, head, tile;     // tile: over all sequences
   int u0, u1;
+  int slot;                // scratch slot of its partial result, or -1: it has all units
   int row0, rows;          // of the sequence's (token, head of the group) rows
   int first, held, q_start;
   TileSpan span;
-  __device__ bool whole() const { return u0 == 0 && u1 == span.n_units; }
-  // Slot of a partial result of workgroup g.
-  __device__ int slot(int g) const { return 2 * g + (u0 == 0 ? 1 : 0); }
 };
 
-// Runs `f` over workgroup g's segments.
+// Fills in what follows from a segment's sequence and tile.
+__device__ __forceinline__ void describe(const PagedView& v, TileShape shape, int tile0, Segment& s) {
+  s.first = plan_array(v.first)[s.seq];
+  s.held = plan_array(v.held)[s.seq];
+  s.q_start = plan_array(v.q_start)[s.seq];
+  s.row0 = (s.tile - tile0) * shape.rows;
+  s.rows = min(shape.rows, plan_array(v.added)[s.seq] * v.group - s.row0);
+  s.span = tile_span(v, s.first + s.row0 / v.group, s.first + (s.row0 + s.rows - 1) / v.group, s.held, shape.unit_keys);
+}
+
+// Tile i of an even plan, in the order (sequence, key head, tile).
+__device__ __forceinline__ void even_tile(const PagedView& v, TileShape shape, int tiles, int i, Segment& s) {
+  const int per_seq = tiles * v.kv_heads, a = i / per_seq, r = i - a * per_seq;
+  s.seq = plan_array(v.active)[a];
+  s.head = r / tiles;
+  const int tile0 = plan_array(v.tile0)[s.seq];
+  s.tile = tile0 + r - s.head * tiles;
+  describe(v, shape, tile0, s);
+}
+
+// Runs `f` over workgroup g's segments (one copy of its code for both dealings).
 template <class F>
 __device__ __forceinline__ void for_segments(const PagedView& v, TileShape shape, int g, F f) {
-  const CONST_AS int32_t* starts = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
+  const CONST_AS int32_t* e = plan_array(&v.header->even.even);
+  const CONST_AS int32_t* w = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
   const CONST_AS int32_t* tile0 = plan_array(v.tile0);
-  int seq = starts[0], head = starts[1], tile = starts[2], unit = starts[3];
-  const int e_seq = starts[4], e_head = starts[5], e_tile = starts[6], e_unit = starts[7];
+  const bool even = shape.even && e[0];
+  int seq = w[0], head = w[1], tile = w[2], unit = w[3];
+  int part = 0, parts = 0;
+  if (even) {
+    const int rounds = e[2], rem = e[3], heads = e[4], tail_len = e[6], tails_per = e[7];
+    const int i0 = (g - heads * rem) * tails_per;
+    parts = rounds + (g < heads * rem ? 1 : tail_len > 0 && i0 < rem ? min(tails_per, rem - i0) : 0);
+  }
   for (;;) {
-    const bool last = seq == e_seq && head == e_head && tile == e_tile;
-    if (last && unit >= e_unit) return;
     Segment s;
-    s.seq = seq;
-    s.head = head;
-    s.tile = tile;
-    s.first = plan_array(v.first)[seq];
-    s.held = plan_array(v.held)[seq];
-    s.q_start = plan_array(v.q_start)[seq];
-    const int t0 = tile0[seq], t1 = tile0[seq + 1];
-    s.row0 = (tile - t0) * shape.rows;
-    s.rows = min(shape.rows, plan_array(v.added)[seq] * v.group - s.row0);
-    s.span = tile_span(v, s.first + s.row0 / v.group, s.first + (s.row0 + s.rows - 1) / v.group, s.held, shape.unit_keys);
-    s.u0 = unit;
-    s.u1 = last ? e_unit : s.span.n_units;
-    f(s);
-    if (last) return;
-    unit = 0;
-    if (++tile == t1) {
-      tile = t0;
-      if (++head == v.kv_heads) {
-        head = 0;
-        tile = t1;
-        do ++seq;
-        while (seq < v.seqs && tile0[seq + 1] == t1);
+    bool last;
+    if (even) {
+      if (part >= parts) return;
+      const int groups = e[1], rounds = e[2], rem = e[3], heads = e[4], head_len = e[5], tail_len = e[6];
+      const int base = rounds * groups, head_groups = heads * rem;
+      int i = part * groups + g;
+      s.u0 = 0;
+      s.u1 = e[8];
+      s.slot = -1;
+      if (part >= rounds && g < head_groups) {
+        const int j = g / rem;
+        i = base + g - j * rem;
+        s.u0 = j * head_len / heads;
+        s.u1 = (j + 1) * head_len / heads;
+        if (heads > 1 || tail_len > 0) s.slot = g;
+      } else if (part >= rounds) {
+        i = base + (g - head_groups) * e[7] + part - rounds;
+        s.u0 = head_len;
+        s.slot = head_groups + i - base;
+      }
+      even_tile(v, shape, e[9], i, s);
+      last = ++part == parts;
+    } else {
+      last = seq == w[4] && head == w[5] && tile == w[6];
+      if (last && unit >= w[7]) return;
+      s.seq = seq;
+      s.head = head;
+      s.tile = tile;
+      describe(v, shape, tile0[seq], s);
+      s.u0 = unit;
+      s.u1 = last ? w[7] : s.span.n_units;
+      s.slot = s.u0 > 0 ? 2 * g : s.u1 < s.span.n_units ? 2 * g + 1 : -1;
+      unit = 0;
+      if (!last && ++tile == tile0[seq + 1]) {
+        const int t1 = tile;
+        tile = tile0[seq];
+        if (++head == v.kv_heads) {
+          head = 0;
+          tile = t1;
+          do ++seq;
+          while (seq < v.seqs && tile0[seq + 1] == t1);
+        }
       }
     }
+    f(s);
+    if (last) return;
   }
 }
 

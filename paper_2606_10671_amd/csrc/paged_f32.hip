@@ -244,9 +244,9 @@ __device__ __forceinline__ void paged_narrow_f32_body(const PagedAttendArgs& a) 
       }
     }
     __syncthreads();
-    const bool whole = s.whole();
+    const bool whole = s.slot < 0;
     bool bad = false;
-    float* slot = v.scratch + size_t(s.slot(g)) * paged_slot_floats(32, D);
+    float* slot = v.scratch + size_t(max(s.slot, 0)) * paged_slot_floats(32, D);
     constexpr int kLanes = D / 4;
     for (int i = tid; i < s.rows * kLanes; i += kNarrowThreads) {
       const int r = i / kLanes, c = 4 * (i % kLanes);
@@ -433,7 +433,7 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
           *reinterpret_cast<f32x4*>(row + 32 * db + 2 * j + 4 * hh) =
               f32x4{o[db][j] * f, o[db][j + 1] * f, o[db][j + 2] * f, o[db][j + 3] * f};
     };
-    if (s.whole()) {
+    if (s.slot < 0) {
       const float inv = 1.0f / l;
       float all = inv;
 #pragma unroll
@@ -447,7 +447,7 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
       const bool bad = __any(r < s.rows && !(__builtin_fabsf(all) < INFINITY));
       if (lane == 0) redo[qw] = bad ? 1 : 0;
     } else {
-      float* slot = v.scratch + size_t(s.slot(g)) * paged_slot_floats(kPagedWideF32.rows, D);
+      float* slot = v.scratch + size_t(max(s.slot, 0)) * paged_slot_floats(kPagedWideF32.rows, D);
       if (r < s.rows) {
         write(slot + size_t(r) * D, 1.0f);
         if (hh == 0) {

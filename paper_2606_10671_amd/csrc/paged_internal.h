@@ -32,11 +32,13 @@ struct TileShape {
   int unit_keys;  // keys of a unit
   int groups;     // workgroups at most: those resident at once
   int overhead;   // key units that a tile costs beside its own: first loads, last results
+  int min_part;   // key units of a part at least
+  int even;       // 1: equal tiles may be dealt evenly (EvenPlan)
 };
-constexpr TileShape kPagedWideBf16 = {256, 64, 256, 4};
-constexpr TileShape kPagedNarrowBf16 = {32, 128, 512, 1};
-constexpr TileShape kPagedWideF32 = {128, 64, 256, 1};
-constexpr TileShape kPagedNarrowF32 = {32, 128, 256, 1};
+constexpr TileShape kPagedWideBf16 = {256, 64, 256, 4, 6, 1};
+constexpr TileShape kPagedNarrowBf16 = {32, 128, 512, 1, 1, 0};
+constexpr TileShape kPagedWideF32 = {128, 64, 256, 1, 2, 1};
+constexpr TileShape kPagedNarrowF32 = {32, 128, 256, 1, 1, 0};
 constexpr int kPagedMinTileRows = 32;
 
 // Floats of a partial result of a tile: O of every row, then row max and row sum.
@@ -44,9 +46,25 @@ __host__ __device__ constexpr size_t paged_slot_floats(int rows, int head_dim) {
   return size_t(rows) * size_t(head_dim + 2);
 }
 
+// Where all tiles of a step have equally many units and all sequences equally
+// many tiles (chunks of a video), the tiles are dealt so that workgroups run the
+// same keys at the same time, which their XCD's L2 then serves: tile i of the
+// first rounds * groups goes to workgroup i % groups, whole; each of the `rem`
+// left is cut into `heads` parts of head_len units together and a tail of
+// tail_len, part j of tile i going to workgroup j * rem + i, the tails to the
+// workgroups left over, tails_per each.  Part j of tile i leaves its partial
+// result in slot j * rem + i, its tail in slot heads * rem + i.
+struct EvenPlan {
+  int32_t even;       // 0: the line above
+  int32_t groups;     // workgroups of a round
+  int32_t rounds, rem, heads, head_len, tail_len, tails_per;
+  int32_t units, tiles;  // units of a tile, tiles of a sequence and head
+};
+
 struct PagedHeader {
   int32_t free;    // free pages
   int32_t groups;  // workgroups with work (attention)
+  EvenPlan even;
 };
 
 // The store as kernels see it.
@@ -66,6 +84,7 @@ struct PagedView {
   int32_t* tile0;      // [seqs + 1] first row tile of each sequence
   int64_t* cost_end;   // [tiles] cost of one head up to and with each tile, in key units
   WorkStart* starts;   // [groups + 1]
+  int32_t* active;     // [seqs] sequences with new tokens (EvenPlan)
   int32_t* joins;      // [groups]: parts of the tile that this workgroup is the first to begin inside, or 0
   uint64_t* redo;      // [tiles][kv_heads]: byte w != 0: rows 32 w.. of the tile have to be worked out again
   float* scratch;      // attention partials
@@ -84,6 +103,11 @@ struct PagedView {
   uint32_t page_magic;  // key / page_tokens = key * page_magic >> page_shift for keys below 2^30
   int32_t page_shift;
 };
+
+// Page of a token (below 2^30).
+__host__ __device__ inline int32_t page_of(const PagedView& v, int32_t key) {
+  return int32_t((uint64_t(uint32_t(key)) * v.page_magic) >> v.page_shift);
+}
 
 // First key of the window of a query at position p, and the end of what it sees.
 __host__ __device__ inline int32_t paged_low(const PagedView& v, int32_t p) {

@@ -30,12 +30,12 @@ __global__ __launch_bounds__(kRotThreads) void rope_kernel(RopeArgs a) {
   constexpr int kElts = BF16 ? 8 : 4;  // elements per 16-byte unit
   const int64_t row0 = int64_t(blockIdx.x) * a.per_block;
   const int n = int(min(int64_t(a.per_block), a.rows - row0));
-  rotary_angles(a.rot, a.pos, row0, n, cs);
-  __syncthreads();
   const int head_units = a.rot.head_dim / kElts, half = head_units / 2;
   const int per_head = HALVES ? half : head_units;
-  const int per_row = a.heads * per_head;
-  for (int i = threadIdx.x; i < n * per_row; i += kRotThreads) {
+  const int per_row = a.heads * per_head, items = n * per_row;
+  rotary_angles(a.rot, a.pos, row0, n, cs);
+  __syncthreads();
+  for (int i = threadIdx.x; i < items; i += kRotThreads) {
     const int t = i / per_row, r = i - t * per_row;
     const int h = r / per_head, u = r - h * per_head;
     const rot_u32x4* src = reinterpret_cast<const rot_u32x4*>(a.x + size_t(row0 + t) * a.x_pitch) + h * head_units + u;
@@ -132,10 +132,7 @@ int fademem_rope_apply(const fademem_rope* rope, int32_t dtype, const int32_t* p
   a.pos = pos;
   a.rows = rows;
   a.heads = heads;
-  const int per_row = int(row * elt / 16);
-  int64_t per = 1024 / per_row;
-  if (per > (rows + 511) / 512) per = (rows + 511) / 512;
-  a.per_block = int(per < 1 ? 1 : per > kRotMaxRows ? kRotMaxRows : per);
+  a.per_block = rows_per_block(rows, int(row * elt / 16), a.rot.pairs);
   const int64_t blocks = (rows + a.per_block - 1) / a.per_block;
   if (blocks > int64_t(0x7fffffff)) return FADEMEM_EINVAL;
   const bool bf16 = dtype == FADEMEM_BF16, halves = a.rot.halves != 0;
