@@ -153,7 +153,7 @@ __global__ void paged_init_kernel(PagedView v, int64_t words, int64_t entries) {
   const int64_t step = int64_t(gridDim.x) * blockDim.x, i0 = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
   if (i0 == 0) {
     v.header->free = int32_t(v.n_pages);
-    v.header->groups = 0;
+    v.header->groups = v.header->tiles = v.header->refused = 0;
     v.q_start[v.seqs] = 0;
   }
   for (int64_t i = i0; i < v.seqs; i += step) {
@@ -364,6 +364,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
     taken = block_scan(uint32_t(need), red_a);
   }
   const bool admitted = ok && code == FADEMEM_OK;
+  const int refused = __syncthreads_or(live && !admitted);
   const int64_t released = going.sum, given = taken.sum;
 
   // Release.
@@ -532,6 +533,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
     int launched = groups;
     if (even && n_tiles > 0) launched = even_plan(int(n_tiles * v.kv_heads), even_units, even_tiles, a.shape, &e);
     v.header->groups = launched;
+    v.header->tiles = int32_t(n_tiles);
+    v.header->refused = refused;
     v.header->even = e;
   }
   __syncthreads();
@@ -810,7 +813,7 @@ int fademem_paged_attend(fademem_paged* c, int32_t layer, const void* q, int64_t
   a.scale = scale == 0.0f ? 1.0f / sqrtf(float(c->cfg.head_dim)) : scale;
   const bool bf16 = c->cfg.dtype == FADEMEM_BF16, narrow = narrow_step(c);
   hipError_t e = bf16 ? launch_paged_bf16(a, narrow, as_stream(stream)) : launch_paged_f32(a, narrow, as_stream(stream));
-  if (e == hipSuccess) e = launch_paged_finish(a, bf16, step_shape(c), as_stream(stream));
+  if (e == hipSuccess) e = launch_paged_finish(a, bf16, step_shape(c), c->max_new, as_stream(stream));
   if (e != hipSuccess) return hip_fail(c, e);
   return finish(c, stream);
 }

@@ -112,107 +112,152 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, 
   if (a.lse && lane == 0) a.lse[size_t(qr.head) * a.rows + qr.row] = (m + log2f(l)) * kLn2;
 }
 
-// grid = (groups at most, chunks of a tile's rows); a block joins kJoinRows rows,
-// a thread four elements of kPer of them, all its loads of two parts in flight.
-constexpr int kJoinRows = 32;
-template <bool BF16, int D>
-__global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAttendArgs a, TileShape shape) {
+// grid = (groups at most, chunks of a tile's rows): a block joins ROWS rows of the
+// tile that workgroup blockIdx.x is the first to begin inside.  Bound by latency:
+// kernel arguments, plan, partial results (beside the sequence's lengths), results.
+// SLICED = false (wide tiles, few parts): a thread takes four elements of several
+// rows, two parts at a time.  SLICED (narrow tiles, up to hundreds of parts): the
+// block's threads share out the parts of ROWS rows, AHEAD of them in flight per
+// thread, and add up through LDS.  Each keeps a running max.
+template <bool BF16, int D, bool SLICED, int ROWS, int AHEAD>
+__global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAttendArgs a, TileShape shape, int rows_used) {
+  constexpr int kLanes = D / 4, kSlices = kFinishThreads / kLanes;  // threads of a row; rows (or parts) side by side
+  constexpr int kPer = SLICED ? ROWS : ROWS / kSlices;  // rows of a thread
   __shared__ float q_s[kFinishWaves][D];
   __shared__ int list[kFinishThreads + 1], n_list;
+  __shared__ float4 o_s[SLICED ? ROWS : 1][SLICED ? kFinishThreads : 1];
+  __shared__ float2 ml_s[SLICED ? ROWS : 1][kSlices];
   const PagedView& v = a.v;
   const int tid = threadIdx.x, wave = tid >> 6, g = blockIdx.x;
-  // Join the tile that workgroup g is the first to begin inside: group g - 1's last
-  // units, then the first units of groups g, g + 1, ...; of an even plan, tile g of
-  // those left over.
-  const EvenPlan even = v.header->even;
+  const CONST_AS int32_t* h = plan_array(&v.header->groups);
+  const CONST_AS int32_t* start = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
+  const int groups = h[0], tiles = h[1], refused = h[2], join = plan_array(v.joins)[g];
+  const int start_seq = start[0], start_head = start[1], start_tile = start[2];
+  const EvenPlan even = {h[3], h[4], h[5], h[6], h[7], h[8], h[9], h[10], h[11], h[12]};
   const bool is_even = shape.even && even.even;
-  const int groups = plan_array(&v.header->groups)[0];
+  // Parts: group g - 1's last units, then the first units of groups g, g + 1, ...; of an even plan, those of tile g
+  // of the tiles left over.
   int parts = 0;
   if (is_even) {
     if (g < even.rem) parts = even.heads + (even.tail_len > 0 ? 1 : 0);
   } else if (g > 0 && g < groups) {
-    parts = plan_array(v.joins)[g];
+    parts = join;
   }
+  const int64_t jobs = blockIdx.y == 0 ? int64_t(tiles) * v.kv_heads : 0;
+  uint64_t mark = int64_t(g) * kFinishThreads + tid < jobs ? v.redo[int64_t(g) * kFinishThreads + tid] : 0;
   Segment mine = {};
   bool again = false;
   if (parts > 1) {
     Segment s;
-    if (is_even) {
-      even_tile(v, shape, even.tiles, even.rounds * even.groups + g, s);
-    } else {
-      const WorkStart w = v.starts[g];
-      s.seq = w.seq;
-      s.head = w.head;
-      s.tile = w.tile;
-      describe(v, shape, v.tile0[w.seq], s);
-    }
     const int slot0 = is_even ? g : 2 * g - 1, slot1 = is_even ? g + even.rem : 2 * g, step = is_even ? even.rem : 2;
-    constexpr int kLanes = D / 4, kStep = kFinishThreads / kLanes, kPer = kJoinRows / kStep;
-    const int c = 4 * (tid % kLanes), r0 = blockIdx.y * kJoinRows + tid / kLanes;
+    const int lane = tid % kLanes, c = 4 * lane, slice = tid / kLanes, base = blockIdx.y * ROWS;
     const size_t slot = paged_slot_floats(shape.rows, D);
     auto part = [&](int p) { return v.scratch + size_t(p == 0 ? slot0 : slot1 + (p - 1) * step) * slot; };
+    auto find = [&] {
+      if (is_even) {
+        even_tile(v, shape, even.tiles, even.rounds * even.groups + g, s);
+      } else {
+        s.seq = start_seq;
+        s.head = start_head;
+        s.tile = start_tile;
+        describe(v, shape, plan_array(v.tile0)[s.seq], s);
+      }
+    };
     bool bad = false;
     auto store = [&](int r, float m, float l, const float4& o) {
-      const QueryRow q = query_row(v, s, r);
+      const int t = (s.row0 + r) / v.group, head = s.head * v.group + s.row0 + r - t * v.group, row = s.q_start + t;
       const float inv = 1.0f / l;
-      char* out = a.out + size_t(q.row) * a.out_pitch + (size_t(q.head) * D + c) * (BF16 ? 2 : 4);
+      char* out = a.out + size_t(row) * a.out_pitch + (size_t(head) * D + c) * (BF16 ? 2 : 4);
       if constexpr (BF16) {
         const uint2 y = {round_pair(o.x * inv, o.y * inv), round_pair(o.z * inv, o.w * inv)};
         *reinterpret_cast<uint2*>(out) = y;
       } else {
         *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
       }
-      if (a.lse && c == 0) a.lse[size_t(q.head) * a.rows + q.row] = (m + log2f(l)) * kLn2;
+      if (a.lse && c == 0) a.lse[size_t(head) * a.rows + row] = (m + log2f(l)) * kLn2;
       const float sum = (o.x + o.y) + (o.z + o.w) + inv;
       bad = bad || !(__builtin_fabsf(sum) < INFINITY);
     };
-    if (parts == 2) {
-      const float *x = part(0), *y = part(1);
-      float4 ox[kPer], oy[kPer];
-      float mx[kPer], my[kPer], lx[kPer], ly[kPer];
+    // Rows of this thread, and its parts: all of them, or every kSlices-th.  Rows below the host's bound are read
+    // before the sequence's lengths are known.
+    auto row_of = [&](int i) { return SLICED ? base + i : base + slice + i * kSlices; };
+    float4 o[kPer];
+    float m[kPer], l[kPer];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int r = min(r0 + i * kStep, s.rows - 1);
-        ox[i] = *reinterpret_cast<const float4*>(x + size_t(r) * D + c);
-        oy[i] = *reinterpret_cast<const float4*>(y + size_t(r) * D + c);
-        mx[i] = x[shape.rows * D + r];
-        my[i] = y[shape.rows * D + r];
-        lx[i] = x[shape.rows * (D + 1) + r];
-        ly[i] = y[shape.rows * (D + 1) + r];
-      }
+    for (int i = 0; i < kPer; ++i) {
+      o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      m[i] = -INFINITY;
+      l[i] = 0.0f;
+    }
+    constexpr int kStep = SLICED ? kSlices : 1;
+    for (int p0 = SLICED ? slice : 0; p0 < parts; p0 += kStep * AHEAD) {
+      float4 y[AHEAD][kPer];
+      float my[AHEAD][kPer], ly[AHEAD][kPer];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int r = r0 + i * kStep;
-        if (r >= s.rows) break;
-        const float m = fmaxf(mx[i], my[i]), ref = m == -INFINITY ? 0.0f : m;
-        const float f = exp2f(mx[i] - ref), h = exp2f(my[i] - ref);
-        store(r, m, f * lx[i] + h * ly[i],
-              make_float4(f * ox[i].x + h * oy[i].x, f * ox[i].y + h * oy[i].y, f * ox[i].z + h * oy[i].z,
-                          f * ox[i].w + h * oy[i].w));
-      }
-    } else {
-      for (int i = 0; i < kPer; ++i) {
-        const int r = r0 + i * kStep;
-        if (r >= s.rows) break;
-        const int mi = shape.rows * D + r, li = mi + shape.rows;
-        float m = -INFINITY;
-#pragma unroll 8
-        for (int p = 0; p < parts; ++p) m = fmaxf(m, part(p)[mi]);
-        const float ref = m == -INFINITY ? 0.0f : m;
-        float l = 0.0f;
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-        for (int p = 0; p < parts; ++p) {
-          const float* x = part(p);
-          const float f = exp2f(x[mi] - ref);
-          const float4 y = *reinterpret_cast<const float4*>(x + size_t(r) * D + c);
-          l += f * x[li];
-          o.x += f * y.x;
-          o.y += f * y.y;
-          o.z += f * y.z;
-          o.w += f * y.w;
+      for (int j = 0; j < AHEAD; ++j) {
+        const int p = p0 + j * kStep;
+        const float* x = part(min(p, parts - 1));
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int row = min(row_of(i), rows_used - 1);
+          y[j][i] = *reinterpret_cast<const float4*>(x + size_t(row) * D + c);
+          my[j][i] = p < parts ? x[shape.rows * D + row] : -INFINITY;
+          ly[j][i] = x[shape.rows * (D + 1) + row];
         }
-        store(r, m, l, o);
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        float top = m[i];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) top = __builtin_elementwise_maximum(top, my[j][i]);
+        const float ref = top == -INFINITY ? 0.0f : top, f0 = exp2f(m[i] - ref);
+        m[i] = top;
+        l[i] *= f0;
+        o[i] = make_float4(o[i].x * f0, o[i].y * f0, o[i].z * f0, o[i].w * f0);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          if (p0 + j * kStep >= parts) continue;
+          const float f = exp2f(my[j][i] - ref);
+          l[i] += f * ly[j][i];
+          o[i].x += f * y[j][i].x;
+          o[i].y += f * y[j][i].y;
+          o[i].z += f * y[j][i].z;
+          o[i].w += f * y[j][i].w;
+        }
+      }
+    }
+    find();
+    if constexpr (!SLICED) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (row_of(i) < s.rows) store(row_of(i), m[i], l[i], o[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        o_s[i][tid] = o[i];
+        if (lane == 0) ml_s[i][slice] = make_float2(m[i], l[i]);
+      }
+      __syncthreads();
+      for (int i = tid; i < min(ROWS, s.rows - base) * kLanes; i += kFinishThreads) {  // kLanes divides the step
+        const int r = i / kLanes;
+        float top = ml_s[r][0].x;
+#pragma unroll
+        for (int k = 1; k < kSlices; ++k) top = __builtin_elementwise_maximum(top, ml_s[r][k].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float ls = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kSlices; ++k) {
+          const float2 ml = ml_s[r][k];
+          const float f = exp2f(ml.x - ref);
+          const float4 z = o_s[r][k * kLanes + lane];
+          ls += f * ml.y;
+          sum.x += f * z.x;
+          sum.y += f * z.y;
+          sum.z += f * z.z;
+          sum.w += f * z.w;
+        }
+        store(base + r, top, ls, sum);
       }
     }
     again = __syncthreads_or(bad);
@@ -221,9 +266,8 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
 
   // Rows again: this block's, if joining them gave something that is not finite,
   // and rows of whole tiles that the attention marked.
-  const int64_t jobs = blockIdx.y == 0 ? int64_t(v.tile0[v.seqs]) * v.kv_heads : 0;
   for (int64_t j0 = int64_t(g) * kFinishThreads; again || j0 < jobs; j0 += int64_t(gridDim.x) * kFinishThreads) {
-    const uint64_t mark = j0 + tid < jobs ? v.redo[j0 + tid] : 0;
+    if (j0 > int64_t(g) * kFinishThreads) mark = j0 + tid < jobs ? v.redo[j0 + tid] : 0;
     if (!__syncthreads_or(mark != 0) && !again) continue;
     if (tid == 0) {
       n_list = again;
@@ -234,7 +278,7 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
     __syncthreads();
     for (int i = 0; i < n_list; ++i) {
       Segment s = mine;
-      int r0 = blockIdx.y * kJoinRows, r1 = min(r0 + kJoinRows, mine.rows);
+      int r0 = blockIdx.y * ROWS, r1 = min(r0 + ROWS, mine.rows);
       uint64_t marks = ~uint64_t(0);
       if (list[i] >= 0) {
         const int64_t j = j0 + list[i];
@@ -258,7 +302,7 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
     again = false;
     __syncthreads();
   }
-  if (blockIdx.y > 0) return;
+  if (blockIdx.y > 0 || !refused) return;
 
   // Rows of sequences that were not admitted.
   for (int s = g; s < v.seqs; s += gridDim.x) {
@@ -277,11 +321,23 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
 
 }  // namespace
 
-hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, hipStream_t stream) {
-  auto kernel = a.v.head_dim == 128 ? (bf16 ? paged_finish_kernel<true, 128> : paged_finish_kernel<false, 128>)
-                                    : (bf16 ? paged_finish_kernel<true, 64> : paged_finish_kernel<false, 64>);
-  hipLaunchKernelGGL(kernel, dim3(unsigned(shape.groups), unsigned(shape.rows / kJoinRows)), dim3(kFinishThreads), 0, stream, a,
-                     shape);
+hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, int64_t max_new, hipStream_t stream) {
+  const int64_t most = max_new * a.v.group;  // rows of a sequence
+  const int rows_used = int(most < 1 ? 1 : most < shape.rows ? most : shape.rows);
+  // Narrow tiles: a block per row or, from five rows on, per four (32 rows of 32 tiles over 8000 tokens: a block per
+  // row 104 us a call, per four 64); wide ones: a block per 32.
+  const bool d128 = a.v.head_dim == 128, narrow = shape.rows == kPagedMinTileRows;
+  const int rows = !narrow ? 32 : rows_used <= 4 ? 1 : 4;
+  void (*kernel)(PagedAttendArgs, TileShape, int);
+  if (d128) {
+    if (bf16) kernel = !narrow ? paged_finish_kernel<true, 128, false, 32, 2> : rows == 1 ? paged_finish_kernel<true, 128, true, 1, 4> : paged_finish_kernel<true, 128, true, 4, 2>;
+    else kernel = !narrow ? paged_finish_kernel<false, 128, false, 32, 2> : rows == 1 ? paged_finish_kernel<false, 128, true, 1, 4> : paged_finish_kernel<false, 128, true, 4, 2>;
+  } else {
+    if (bf16) kernel = !narrow ? paged_finish_kernel<true, 64, false, 32, 2> : rows == 1 ? paged_finish_kernel<true, 64, true, 1, 4> : paged_finish_kernel<true, 64, true, 4, 2>;
+    else kernel = !narrow ? paged_finish_kernel<false, 64, false, 32, 2> : rows == 1 ? paged_finish_kernel<false, 64, true, 1, 4> : paged_finish_kernel<false, 64, true, 4, 2>;
+  }
+  hipLaunchKernelGGL(kernel, dim3(unsigned(shape.groups), unsigned((rows_used + rows - 1) / rows)), dim3(kFinishThreads), 0,
+                     stream, a, shape, rows_used);
   return hipGetLastError();
 }
 

@@ -36,7 +36,7 @@ struct TileShape {
   int even;       // 1: equal tiles may be dealt evenly (EvenPlan)
 };
 constexpr TileShape kPagedWideBf16 = {256, 64, 256, 4, 6, 1};
-constexpr TileShape kPagedNarrowBf16 = {32, 128, 512, 1, 1, 0};
+constexpr TileShape kPagedNarrowBf16 = {32, 128, 512, 1, 2, 0};
 constexpr TileShape kPagedWideF32 = {128, 64, 256, 1, 2, 1};
 constexpr TileShape kPagedNarrowF32 = {32, 128, 256, 1, 1, 0};
 constexpr int kPagedMinTileRows = 32;
@@ -64,6 +64,8 @@ struct EvenPlan {
 struct PagedHeader {
   int32_t free;    // free pages
   int32_t groups;  // workgroups with work (attention)
+  int32_t tiles;   // row tiles of the step
+  int32_t refused; // 1: some sequence was not admitted
   EvenPlan even;
 };
 
@@ -155,6 +157,6 @@ struct PagedAttendArgs {
 // an infinity or NaN of a hidden key may have reached (paged_attend.hip).
 hipError_t launch_paged_bf16(const PagedAttendArgs& a, bool narrow, hipStream_t stream);
 hipError_t launch_paged_f32(const PagedAttendArgs& a, bool narrow, hipStream_t stream);
-hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, hipStream_t stream);
+hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, int64_t max_new, hipStream_t stream);
 
 }  // namespace fademem
