@@ -94,7 +94,7 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   v->tile0 = reinterpret_cast<int32_t*>(take((seqs + 1) * 4));
   v->cost_end = reinterpret_cast<int64_t*>(take(uint64_t(max_tiles(c)) * 8));
   v->starts = reinterpret_cast<WorkStart*>(take((kPagedMaxGroups + 1) * sizeof(WorkStart)));
-  v->active = reinterpret_cast<int32_t*>(take(seqs * 4));
+  v->tile_seq = reinterpret_cast<int32_t*>(take(uint64_t(max_tiles(c)) * 4));
   v->joins = reinterpret_cast<int32_t*>(take(kPagedMaxGroups * sizeof(int32_t)));
   v->redo = reinterpret_cast<uint64_t*>(take((unsigned __int128)uint64_t(max_tiles(c)) * unsigned(c.kv_heads) * 8));
   const size_t wide_slots = 2 * size_t(wide.groups) * paged_slot_floats(wide.rows, c.head_dim);
@@ -138,7 +138,7 @@ bool valid_config(const fademem_paged_config* c) {
   if (c->dtype != FADEMEM_F32 && c->dtype != FADEMEM_BF16) return false;
   if (c->page_tokens < 1 || c->page_tokens > 65536 || c->pages < 1 || c->pages > (int64_t(1) << 24)) return false;
   if (c->max_tokens < 1 || c->max_tokens > most || c->max_rows < 1 || c->max_rows > (int64_t(1) << 24)) return false;
-  if (c->max_rows * (c->heads / c->kv_heads) > most) return false;
+  if (c->max_rows * (c->heads / c->kv_heads) > most || max_tiles(*c) * c->kv_heads > most) return false;
   if (c->block_tokens < 1 || c->block_tokens > most || c->window < 0 || c->window > most) return false;
   if (c->sinks < 0) return false;
   if (c->grid_h < 1 || c->grid_w < 1 || int64_t(c->grid_h) * c->grid_w > most) return false;
@@ -269,11 +269,10 @@ __device__ __forceinline__ void write_row(const PagedView& v, int64_t i, bool li
 // head part's own; tails that take less than two units off every head part are
 // left out.
 constexpr int kMinTailSaves = 2;
-__device__ int even_plan(int total, int units, int tiles, TileShape shape, EvenPlan* e) {
+__device__ int even_plan(int total, int units, TileShape shape, EvenPlan* e) {
   e->even = 1;
   e->groups = shape.groups;
   e->units = units;
-  e->tiles = tiles;
   e->rounds = total / shape.groups;
   e->rem = total - e->rounds * shape.groups;
   e->heads = e->tails_per = 1;
@@ -443,13 +442,10 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   // The attention's work: row tiles, their costs in key units, where each workgroup starts.
   const int G = v.group;
   const int tiles_s = (int(fresh) * G + a.shape.rows - 1) / a.shape.rows;
-  const Scan tiles = block_scan(tiles_s, red_b), live_seqs = block_scan(fresh > 0, red_a);
+  const Scan tiles = block_scan(tiles_s, red_b);
   const int64_t n_tiles = tiles.sum;
   if (live) {
-    if (fresh > 0) {
-      v.active[live_seqs.x - 1] = s;
-      if (live_seqs.x == 1) even_tiles = tiles_s;
-    }
+    if (tiles_s > 0 && tiles.x == tiles_s) even_tiles = tiles_s;
     pre[s] = tiles.x - tiles_s;
     v.tile0[s] = int32_t(tiles.x - tiles_s);
     r1_lo[s] = int32_t(k);
@@ -470,24 +466,26 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
     const int64_t t = one_each ? pre[min(s, seqs)] : t0 + tid;
     const bool has = one_each ? tiles_s > 0 : t < n_tiles;
     int64_t cost = 0;
+    int q = 0;
     if (has) {
-      const int q = one_each ? s : last_at_most<int64_t>(pre, seqs, t);
+      q = one_each ? s : last_at_most<int64_t>(pre, seqs, t);
       const int first_row = int(t - pre[q]) * a.shape.rows, row1 = min(first_row + a.shape.rows, r2_lo[q] * G);
       const int32_t p = r1_lo[q];
       cost = a.shape.overhead + tile_span(v, p + first_row / G, p + (row1 - 1) / G, p + r2_lo[q], a.shape.unit_keys).n_units;
     }
     const int32_t units = int32_t(cost) - a.shape.overhead;
     if (t == 0) even_units = units;
-    const Scan upto = block_scan(uint32_t(cost), t0 / kPlanThreads % 2 ? red_a : red_b);
+    const Scan upto = block_scan(uint32_t(cost), t0 / kPlanThreads % 2 ? red_b : red_a);
     even = even && (!has || units == even_units);
     if (has) {
       v.cost_end[t] = cost0 + upto.x;
+      v.tile_seq[t] = q;
       if (t < kCostsInLds) cost_s[t] = cost0 + upto.x;
     }
     cost0 += upto.sum;
   }
   __syncthreads();
-  even = __syncthreads_and(even) && n_tiles * v.kv_heads < (int64_t(1) << 30);
+  even = __syncthreads_and(even);
   const int64_t all = cost0 * v.kv_heads;
   const int min_cost = a.shape.overhead + a.shape.min_part;
   int groups = all >= int64_t(a.shape.groups) * min_cost ? a.shape.groups : (int(all) + min_cost - 1) / min_cost;
@@ -500,7 +498,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
     __syncthreads();
   }
   if (tid <= groups && groups > 0) {
-    WorkStart w = {seqs, 0, int32_t(n_tiles), 0};
+    WorkStart w = {int32_t(n_tiles) * v.kv_heads, 0};
     if (tid < groups) {
       const int64_t at = int64_t(double(all) * double(tid) / double(groups));  // rises with tid and stays below `all`
       // The last sequence that begins at or before `at`: it has tiles.
@@ -510,19 +508,19 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
         if (base_s[mid] * v.kv_heads <= at) lo = mid;
         else hi = mid;
       }
-      w.seq = lo;
       const int64_t base = base_s[lo], per_head = base_s[lo + 1] - base, local = at - base * v.kv_heads;
-      w.head = int32_t(double(local) / double(per_head));  // within one of the quotient; made exact
-      w.head += (w.head + 1) * per_head <= local ? 1 : 0;
-      w.head -= w.head * per_head > local ? 1 : 0;
-      const int64_t x = base + local - w.head * per_head;  // on the line of the sequence's tiles
-      int64_t t = pre[w.seq], e = pre[w.seq + 1];          // first tile that ends behind x
+      int head = int(double(local) / double(per_head));  // within one of the quotient; made exact
+      head += (head + 1) * per_head <= local ? 1 : 0;
+      head -= head * per_head > local ? 1 : 0;
+      const int64_t x = base + local - head * per_head;  // on the line of the sequence's tiles
+      int64_t t = pre[lo], e = pre[lo + 1];              // first tile that ends behind x
       while (t < e) {
         const int64_t mid = (t + e) >> 1;
         if (cost_end(mid) > x) e = mid;
         else t = mid + 1;
       }
-      w.tile = int32_t(t);
+      const int64_t n = pre[lo + 1] - pre[lo];
+      w.task = int32_t(pre[lo] * v.kv_heads + head * n + t - pre[lo]);
       w.unit = int32_t(max(int64_t(0), x - (t > 0 ? cost_end(t - 1) : 0) - a.shape.overhead));
     }
     v.starts[tid] = w;
@@ -531,7 +529,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   if (tid == 0) {
     EvenPlan e = {};
     int launched = groups;
-    if (even && n_tiles > 0) launched = even_plan(int(n_tiles * v.kv_heads), even_units, even_tiles, a.shape, &e);
+    if (even && n_tiles > 0) launched = even_plan(int(n_tiles * v.kv_heads), even_units, a.shape, &e);
     v.header->groups = launched;
     v.header->tiles = int32_t(n_tiles);
     v.header->refused = refused;
@@ -542,9 +540,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
   if (tid < groups) {
     const WorkStart w = starts[tid];
     int parts = 0;
-    if (w.unit > 0 && (starts[tid - 1].unit == 0 || starts[tid - 1].tile != w.tile || starts[tid - 1].head != w.head)) {
+    if (w.unit > 0 && (starts[tid - 1].unit == 0 || starts[tid - 1].task != w.task)) {
       parts = 2;
-      for (int i = tid + 1; i < groups && starts[i].unit > 0 && starts[i].tile == w.tile && starts[i].head == w.head; ++i)
+      for (int i = tid + 1; i < groups && starts[i].unit > 0 && starts[i].task == w.task; ++i)
         ++parts;
     }
     v.joins[tid] = parts;

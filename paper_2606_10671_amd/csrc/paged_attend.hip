@@ -132,8 +132,8 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
   const CONST_AS int32_t* h = plan_array(&v.header->groups);
   const CONST_AS int32_t* start = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
   const int groups = h[0], tiles = h[1], refused = h[2], join = plan_array(v.joins)[g];
-  const int start_seq = start[0], start_head = start[1], start_tile = start[2];
-  const EvenPlan even = {h[3], h[4], h[5], h[6], h[7], h[8], h[9], h[10], h[11], h[12]};
+  const int start_task = start[0];
+  const EvenPlan even = {h[3], h[4], h[5], h[6], h[7], h[8], h[9], h[10], h[11]};
   const bool is_even = shape.even && even.even;
   // Parts: group g - 1's last units, then the first units of groups g, g + 1, ...; of an even plan, those of tile g
   // of the tiles left over.
@@ -154,14 +154,8 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
     const size_t slot = paged_slot_floats(shape.rows, D);
     auto part = [&](int p) { return v.scratch + size_t(p == 0 ? slot0 : slot1 + (p - 1) * step) * slot; };
     auto find = [&] {
-      if (is_even) {
-        even_tile(v, shape, even.tiles, even.rounds * even.groups + g, s);
-      } else {
-        s.seq = start_seq;
-        s.head = start_head;
-        s.tile = start_tile;
-        describe(v, shape, plan_array(v.tile0)[s.seq], s);
-      }
+      s.task = is_even ? even.rounds * even.groups + g : start_task;
+      describe(v, shape, s);
     };
     bool bad = false;
     auto store = [&](int r, float m, float l, const float4& o) {
@@ -281,20 +275,11 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
       int r0 = blockIdx.y * ROWS, r1 = min(r0 + ROWS, mine.rows);
       uint64_t marks = ~uint64_t(0);
       if (list[i] >= 0) {
-        const int64_t j = j0 + list[i];
-        s.tile = int(j / v.kv_heads);
-        s.head = int(j - int64_t(s.tile) * v.kv_heads);
-        int lo = 0, hi = v.seqs;  // the last sequence whose tiles begin at or before it
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (v.tile0[mid] <= s.tile) lo = mid;
-          else hi = mid;
-        }
-        s.seq = lo;
-        describe(v, shape, v.tile0[lo], s);
+        s.task = int(j0) + list[i];
+        describe(v, shape, s);
         r0 = 0;
         r1 = s.rows;
-        marks = v.redo[j];
+        marks = v.redo[s.task];
       }
       for (int r = r0 + wave; r < r1; r += kFinishWaves)
         if ((marks >> (8 * (r >> 5))) & 0xff) attend_row<BF16, D>(a, s.seq, query_row(v, s, r), q_s[wave]);

@@ -98,6 +98,7 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
   __shared__ __attribute__((aligned(16))) char k_lds[kNarrowWaves * kBuf];
   __shared__ __attribute__((aligned(16))) char v_lds[kNarrowWaves * kBuf];
   __shared__ float m_s[kNarrowWaves][32], l_s[kNarrowWaves][32];
+  __shared__ SegmentList segments;
   const PagedView& v = a.v;
   const int groups = plan_array(&v.header->groups)[0];
   if (int(blockIdx.x) >= groups) return;
@@ -112,7 +113,7 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
   const size_t v_off = size_t(v.kv_heads) * P * D * 2;  // from a key's row to its value's
   PageBatch pages_under(v);
 
-  for_segments(v, kPagedNarrowBf16, g, [&](const Segment& s) {
+  for_segments(v, kPagedNarrowBf16, g, segments, [&](const Segment& s) {
     const QueryRow qr = query_row(v, s, min(l32, s.rows - 1));
     bf16x8 qf[R::KB];
     {
@@ -296,7 +297,7 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
       }
     }
     bad = __syncthreads_or(bad);
-    if (s.u0 == 0 && tid == 0) v.redo[size_t(s.tile) * v.kv_heads + s.head] = whole && bad ? ~uint64_t(0) : 0;
+    if (s.u0 == 0 && tid == 0) v.redo[s.task] = whole && bad ? ~uint64_t(0) : 0;
   });
 }
 
@@ -331,6 +332,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
   __shared__ __attribute__((aligned(16))) char v_lds2[kTileBytes];
   char* const kbuf[3] = {k_lds0, k_lds1, k_lds2};
   char* const vbuf[3] = {v_lds0, v_lds1, v_lds2};
+  __shared__ SegmentList segments;
   const PagedView& v = a.v;
   const int groups = plan_array(&v.header->groups)[0];
   if (int(blockIdx.x) >= groups) return;
@@ -359,7 +361,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
     ld_voff[i] = uint32_t(ld_row(i) * D * 2) + ld_vch(i);
   }
 
-  for_segments(v, kPagedWideBf16, g, [&](const Segment& s) {
+  for_segments(v, kPagedWideBf16, g, segments, [&](const Segment& s) {
     const CONST_AS int32_t* table = plan_array(v.table + size_t(s.seq) * v.width);
     const char* pages = a.pages + size_t(s.head) * P * D * 2;
     const int n_sink = s.span.n_sink, end = s.span.end, from = s.span.from, sinks = s.span.sinks;
@@ -433,7 +435,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
           load_tile(t + 2, b == 0 ? kbuf[0] : b == 1 ? kbuf[1] : kbuf[2], b == 0 ? vbuf[0] : b == 1 ? vbuf[1] : vbuf[2]);
         b = b == 2 ? 0 : b + 1;
       }
-      if (s.u0 == 0 && lane == 0) reinterpret_cast<uint8_t*>(v.redo + size_t(s.tile) * v.kv_heads + s.head)[wave] = 0;
+      if (s.u0 == 0 && lane == 0) reinterpret_cast<uint8_t*>(v.redo + s.task)[wave] = 0;
       return;
     }
 
@@ -677,7 +679,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
         }
       if (a.lse && hh == 0 && r < s.rows) a.lse[size_t(qr.head) * a.rows + qr.row] = (m * c2 + __log2f(l)) * kLn2;
       const bool bad = __any(r < s.rows && !(__builtin_fabsf(all) < INFINITY));
-      if (lane == 0) reinterpret_cast<uint8_t*>(v.redo + size_t(s.tile) * v.kv_heads + s.head)[wave] = bad ? 1 : 0;
+      if (lane == 0) reinterpret_cast<uint8_t*>(v.redo + s.task)[wave] = bad ? 1 : 0;
     } else {
       float* slot = v.scratch + size_t(max(s.slot, 0)) * paged_slot_floats(kPagedWideBf16.rows, D);
       if (r < s.rows) {
@@ -693,7 +695,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
           slot[256 * (D + 1) + r] = l;
         }
       }
-      if (s.u0 == 0 && lane == 0) reinterpret_cast<uint8_t*>(v.redo + size_t(s.tile) * v.kv_heads + s.head)[wave] = 0;
+      if (s.u0 == 0 && lane == 0) reinterpret_cast<uint8_t*>(v.redo + s.task)[wave] = 0;
     }
   });
 }

@@ -37,98 +37,122 @@ __device__ __forceinline__ void wait_lds() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Units [u0, u1) of a row tile: the work of one segment.
+// Units [u0, u1) of a task: the work of one segment.
 struct Segment {
-  int seq, head, tile;     // tile: over all sequences
   int u0, u1;
   int slot;                // scratch slot of its partial result, or -1: it has all units
+  int task, seq, head;
   int row0, rows;          // of the sequence's (token, head of the group) rows
   int first, held, q_start;
   TileSpan span;
 };
 
-// Fills in what follows from a segment's sequence and tile.
-__device__ __forceinline__ void describe(const PagedView& v, TileShape shape, int tile0, Segment& s) {
+// What follows from a segment's task.
+__device__ __forceinline__ void describe(const PagedView& v, TileShape shape, Segment& s) {
+  s.seq = plan_array(v.tile_seq)[s.task / v.kv_heads];  // a sequence's tasks are kv_heads times its tiles, as is their first
+  const int t0 = plan_array(v.tile0)[s.seq], tiles = plan_array(v.tile0)[s.seq + 1] - t0;
   s.first = plan_array(v.first)[s.seq];
   s.held = plan_array(v.held)[s.seq];
   s.q_start = plan_array(v.q_start)[s.seq];
-  s.row0 = (s.tile - tile0) * shape.rows;
-  s.rows = min(shape.rows, plan_array(v.added)[s.seq] * v.group - s.row0);
+  const int added = plan_array(v.added)[s.seq], r = s.task - t0 * v.kv_heads;
+  s.head = r / tiles;
+  s.row0 = (r - s.head * tiles) * shape.rows;
+  s.rows = min(shape.rows, added * v.group - s.row0);
   s.span = tile_span(v, s.first + s.row0 / v.group, s.first + (s.row0 + s.rows - 1) / v.group, s.held, shape.unit_keys);
 }
 
-// Tile i of an even plan, in the order (sequence, key head, tile).
-__device__ __forceinline__ void even_tile(const PagedView& v, TileShape shape, int tiles, int i, Segment& s) {
-  const int per_seq = tiles * v.kv_heads, a = i / per_seq, r = i - a * per_seq;
-  s.seq = plan_array(v.active)[a];
-  s.head = r / tiles;
-  const int tile0 = plan_array(v.tile0)[s.seq];
-  s.tile = tile0 + r - s.head * tiles;
-  describe(v, shape, tile0, s);
+// A workgroup's segments, described by its threads side by side, kSegBatch at a
+// time, in LDS: walking the plan's arrays segment by segment took three dependent
+// reads each time.
+constexpr int kSegBatch = 64;
+struct SegmentList {
+  int32_t x[kSegBatch][16];
+};
+
+// Segments of workgroup g.
+__device__ __forceinline__ int count_segments(const PagedView& v, TileShape shape, int g) {
+  const CONST_AS int32_t* e = plan_array(&v.header->even.even);
+  if (shape.even && e[0]) {
+    const int rounds = e[2], rem = e[3], heads = e[4], tail_len = e[6], tails_per = e[7], i0 = (g - heads * rem) * tails_per;
+    return rounds + (g < heads * rem ? 1 : tail_len > 0 && i0 < rem ? min(tails_per, rem - i0) : 0);
+  }
+  const CONST_AS int32_t* w = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
+  return w[2] - w[0] + (w[3] > 0 && (w[2] > w[0] || w[3] > w[1]) ? 1 : 0);
 }
 
-// Runs `f` over workgroup g's segments (one copy of its code for both dealings).
-template <class F>
-__device__ __forceinline__ void for_segments(const PagedView& v, TileShape shape, int g, F f) {
+// Describes segments first .. first + kSegBatch - 1 of `n`; a barrier has to follow.
+__device__ __forceinline__ void list_segments(const PagedView& v, TileShape shape, int g, int first, int n,
+                                              SegmentList& list) {
+  const int i = int(threadIdx.x), k = first + i;
+  if (i >= kSegBatch || k >= n) return;
+  Segment s;
   const CONST_AS int32_t* e = plan_array(&v.header->even.even);
-  const CONST_AS int32_t* w = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
-  const CONST_AS int32_t* tile0 = plan_array(v.tile0);
-  const bool even = shape.even && e[0];
-  int seq = w[0], head = w[1], tile = w[2], unit = w[3];
-  int part = 0, parts = 0;
-  if (even) {
-    const int rounds = e[2], rem = e[3], heads = e[4], tail_len = e[6], tails_per = e[7];
-    const int i0 = (g - heads * rem) * tails_per;
-    parts = rounds + (g < heads * rem ? 1 : tail_len > 0 && i0 < rem ? min(tails_per, rem - i0) : 0);
-  }
-  for (;;) {
-    Segment s;
-    bool last;
-    if (even) {
-      if (part >= parts) return;
-      const int groups = e[1], rounds = e[2], rem = e[3], heads = e[4], head_len = e[5], tail_len = e[6];
-      const int base = rounds * groups, head_groups = heads * rem;
-      int i = part * groups + g;
-      s.u0 = 0;
-      s.u1 = e[8];
-      s.slot = -1;
-      if (part >= rounds && g < head_groups) {
-        const int j = g / rem;
-        i = base + g - j * rem;
-        s.u0 = j * head_len / heads;
-        s.u1 = (j + 1) * head_len / heads;
-        if (heads > 1 || tail_len > 0) s.slot = g;
-      } else if (part >= rounds) {
-        i = base + (g - head_groups) * e[7] + part - rounds;
-        s.u0 = head_len;
-        s.slot = head_groups + i - base;
-      }
-      even_tile(v, shape, e[9], i, s);
-      last = ++part == parts;
-    } else {
-      last = seq == w[4] && head == w[5] && tile == w[6];
-      if (last && unit >= w[7]) return;
-      s.seq = seq;
-      s.head = head;
-      s.tile = tile;
-      describe(v, shape, tile0[seq], s);
-      s.u0 = unit;
-      s.u1 = last ? w[7] : s.span.n_units;
-      s.slot = s.u0 > 0 ? 2 * g : s.u1 < s.span.n_units ? 2 * g + 1 : -1;
-      unit = 0;
-      if (!last && ++tile == tile0[seq + 1]) {
-        const int t1 = tile;
-        tile = tile0[seq];
-        if (++head == v.kv_heads) {
-          head = 0;
-          tile = t1;
-          do ++seq;
-          while (seq < v.seqs && tile0[seq + 1] == t1);
-        }
-      }
+  s.u0 = 0;
+  s.slot = -1;
+  if (shape.even && e[0]) {
+    const int groups = e[1], rounds = e[2], rem = e[3], heads = e[4], head_len = e[5], tail_len = e[6];
+    const int base = rounds * groups, head_groups = heads * rem;
+    s.task = k * groups + g;
+    s.u1 = e[8];
+    if (k >= rounds && g < head_groups) {
+      const int j = g / rem;
+      s.task = base + g - j * rem;
+      s.u0 = j * head_len / heads;
+      s.u1 = (j + 1) * head_len / heads;
+      if (heads > 1 || tail_len > 0) s.slot = g;
+    } else if (k >= rounds) {
+      s.task = base + (g - head_groups) * e[7] + k - rounds;
+      s.u0 = head_len;
+      s.slot = head_groups + s.task - base;
     }
-    f(s);
-    if (last) return;
+    describe(v, shape, s);
+  } else {
+    const CONST_AS int32_t* w = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
+    s.task = w[0] + k;
+    describe(v, shape, s);
+    if (k == 0) s.u0 = w[1];
+    s.u1 = s.task == w[2] ? w[3] : s.span.n_units;
+    s.slot = s.u0 > 0 ? 2 * g : s.u1 < s.span.n_units ? 2 * g + 1 : -1;
+  }
+  const int32_t x[16] = {s.u0,    s.u1,   s.slot,    s.task,        s.seq,         s.head,     s.row0,      s.rows,
+                         s.first, s.held, s.q_start, s.span.n_sink, s.span.n_units, s.span.from, s.span.end, s.span.sinks};
+#pragma unroll
+  for (int j = 0; j < 16; ++j) list.x[i][j] = x[j];
+}
+
+// Segment i of the list, in scalar registers.
+__device__ __forceinline__ Segment read_segment(const SegmentList& list, int i) {
+  const int32_t x = list.x[i][threadIdx.x & 15];
+  auto get = [&](int j) { return int(__builtin_amdgcn_readlane(x, j)); };
+  Segment s;
+  s.u0 = get(0);
+  s.u1 = get(1);
+  s.slot = get(2);
+  s.task = get(3);
+  s.seq = get(4);
+  s.head = get(5);
+  s.row0 = get(6);
+  s.rows = get(7);
+  s.first = get(8);
+  s.held = get(9);
+  s.q_start = get(10);
+  s.span.n_sink = get(11);
+  s.span.n_units = get(12);
+  s.span.from = get(13);
+  s.span.end = get(14);
+  s.span.sinks = get(15);
+  return s;
+}
+
+// Runs `f` over workgroup g's segments.
+template <class F>
+__device__ __forceinline__ void for_segments(const PagedView& v, TileShape shape, int g, SegmentList& list, F f) {
+  const int n = count_segments(v, shape, g);
+  for (int k0 = 0; k0 < n; k0 += kSegBatch) {
+    __syncthreads();
+    list_segments(v, shape, g, k0, n, list);
+    __syncthreads();
+    for (int i = 0; i < min(kSegBatch, n - k0); ++i) f(read_segment(list, i));
   }
 }
 

@@ -124,6 +124,7 @@ __device__ __forceinline__ void paged_narrow_f32_body(const PagedAttendArgs& a) 
   __shared__ __attribute__((aligned(16))) float k_lds[kNarrowWaves * R::TILE];
   __shared__ __attribute__((aligned(16))) float v_lds[kNarrowWaves * R::TILE];
   __shared__ float m_s[kNarrowWaves][32], l_s[kNarrowWaves][32];
+  __shared__ SegmentList segments;
   const PagedView& v = a.v;
   const int groups = plan_array(&v.header->groups)[0];
   if (int(blockIdx.x) >= groups) return;
@@ -137,7 +138,7 @@ __device__ __forceinline__ void paged_narrow_f32_body(const PagedAttendArgs& a) 
   const size_t v_off = size_t(v.kv_heads) * P * D * 4;
   PageBatch pages_under(v);
 
-  for_segments(v, kPagedNarrowF32, g, [&](const Segment& s) {
+  for_segments(v, kPagedNarrowF32, g, segments, [&](const Segment& s) {
     const QueryRow qr = query_row(v, s, min(l32, s.rows - 1));
     f32x4 q[D / 8];
     {
@@ -278,7 +279,7 @@ __device__ __forceinline__ void paged_narrow_f32_body(const PagedAttendArgs& a) 
       }
     }
     bad = __syncthreads_or(bad);
-    if (s.u0 == 0 && tid == 0) v.redo[size_t(s.tile) * v.kv_heads + s.head] = whole && bad ? ~uint64_t(0) : 0;
+    if (s.u0 == 0 && tid == 0) v.redo[s.task] = whole && bad ? ~uint64_t(0) : 0;
   });
 }
 
@@ -302,6 +303,7 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
   __shared__ __attribute__((aligned(16))) float v_lds0[kObj];
   __shared__ __attribute__((aligned(16))) float k_lds1[kObj];
   __shared__ __attribute__((aligned(16))) float v_lds1[kObj];
+  __shared__ SegmentList segments;
   const PagedView& v = a.v;
   const int groups = plan_array(&v.header->groups)[0];
   if (int(blockIdx.x) >= groups) return;
@@ -313,7 +315,7 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
   const int P = v.page_tokens;
   const size_t v_off = size_t(v.kv_heads) * P * D * 4;
 
-  for_segments(v, kPagedWideF32, g, [&](const Segment& s) {
+  for_segments(v, kPagedWideF32, g, segments, [&](const Segment& s) {
     const int32_t* table = v.table + size_t(s.seq) * v.width;
     const char* pages = a.pages + size_t(s.head) * P * D * 4;
     const bool active = 32 * qw < s.rows;  // the wave has a row
@@ -404,7 +406,7 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
       area[64 * (16 * R::DB + 1)] = l;
     }
     __syncthreads();
-    uint8_t* redo = reinterpret_cast<uint8_t*>(v.redo + size_t(s.tile) * v.kv_heads + s.head);
+    uint8_t* redo = reinterpret_cast<uint8_t*>(v.redo + s.task);
     if (split > 0) {
       if (s.u0 == 0 && lane == 0) redo[4 + qw] = 0;
       return;

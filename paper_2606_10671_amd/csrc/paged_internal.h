@@ -16,14 +16,15 @@ constexpr int kPagedMaxGroups = 512;  // workgroups of one attention launch at m
 // pairs of one sequence and one key head, token-major: row r is token r / G,
 // head r % G of the key head's G query heads, so that a tile of K and V serves
 // all of them.  A tile's keys come in units of `unit_keys`: first the units
-// that cover the sinks, then those that cover the window.  All units of a step
-// lie on one line, ordered by (sequence, key head, tile, unit), each tile with its
-// overhead before it, and the line is dealt to the workgroups in equal runs: a run may end one tile's units, take some
-// tiles whole and begin another's.  Units of a tile that several workgroups
-// share leave partial results in their slots (0: a run's first units, which
-// continue a tile; 1: its last units, which begin one).
+// that cover the sinks, then those that cover the window.  A task is a tile of a
+// key head; tasks are numbered in the order (sequence, key head, tile).  The units
+// of all tasks lie on one line, each task with its overhead before it, and the
+// line is dealt to the workgroups in equal runs: a run may end one task's units,
+// take some tasks whole and begin another's.  Units of a task that several
+// workgroups share leave partial results in their slots (0: a run's first units,
+// which continue a task; 1: its last units, which begin one).
 struct WorkStart {
-  int32_t seq, head, tile, unit;  // tile: over all sequences; unit: within the tile
+  int32_t task, unit;  // unit: within the task
 };
 
 // Tile and key-unit shapes of an attention kernel.
@@ -31,9 +32,9 @@ struct TileShape {
   int rows;       // query rows of a tile
   int unit_keys;  // keys of a unit
   int groups;     // workgroups at most: those resident at once
-  int overhead;   // key units that a tile costs beside its own: first loads, last results
+  int overhead;   // key units that a task costs beside its own: first loads, last results
   int min_part;   // key units of a part at least
-  int even;       // 1: equal tiles may be dealt evenly (EvenPlan)
+  int even;       // 1: equal tasks may be dealt evenly (EvenPlan)
 };
 constexpr TileShape kPagedWideBf16 = {256, 64, 256, 4, 6, 1};
 constexpr TileShape kPagedNarrowBf16 = {32, 128, 512, 1, 2, 0};
@@ -48,17 +49,17 @@ __host__ __device__ constexpr size_t paged_slot_floats(int rows, int head_dim) {
 
 // Where all tiles of a step have equally many units and all sequences equally
 // many tiles (chunks of a video), the tiles are dealt so that workgroups run the
-// same keys at the same time, which their XCD's L2 then serves: tile i of the
+// same keys at the same time, which their XCD's L2 then serves: task i of the
 // first rounds * groups goes to workgroup i % groups, whole; each of the `rem`
 // left is cut into `heads` parts of head_len units together and a tail of
-// tail_len, part j of tile i going to workgroup j * rem + i, the tails to the
+// tail_len, part j of the i-th going to workgroup j * rem + i, the tails to the
 // workgroups left over, tails_per each.  Part j of tile i leaves its partial
 // result in slot j * rem + i, its tail in slot heads * rem + i.
 struct EvenPlan {
   int32_t even;       // 0: the line above
   int32_t groups;     // workgroups of a round
   int32_t rounds, rem, heads, head_len, tail_len, tails_per;
-  int32_t units, tiles;  // units of a tile, tiles of a sequence and head
+  int32_t units;      // of a tile
 };
 
 struct PagedHeader {
@@ -86,9 +87,9 @@ struct PagedView {
   int32_t* tile0;      // [seqs + 1] first row tile of each sequence
   int64_t* cost_end;   // [tiles] cost of one head up to and with each tile, in key units
   WorkStart* starts;   // [groups + 1]
-  int32_t* active;     // [seqs] sequences with new tokens (EvenPlan)
+  int32_t* tile_seq;   // [tiles] sequence of each tile
   int32_t* joins;      // [groups]: parts of the tile that this workgroup is the first to begin inside, or 0
-  uint64_t* redo;      // [tiles][kv_heads]: byte w != 0: rows 32 w.. of the tile have to be worked out again
+  uint64_t* redo;      // [tasks]: byte w != 0: rows 32 w.. of the tile have to be worked out again
   float* scratch;      // attention partials
   char* pages;         // layer 0
   size_t layer_bytes;
