@@ -381,7 +381,7 @@ typedef struct fademem_rope {
 int fademem_rope_init(fademem_rope* rope, int32_t head_dim, int32_t layout, int32_t pairs_t, int32_t pairs_h,
                       int32_t pairs_w, double theta);
 
-/* Rotate `rows` rows of `heads` heads: y[i][h] = x[i][h] turned to position
+/* Rotate `rows` rows (at most 2^23) of `heads` heads: y[i][h] = x[i][h] turned to position
  * pos[i] (device int32 [rows][3]; any int32 values).  x and y: device, rows
  * x_stride / y_stride elements apart (>= heads * head_dim, a multiple of 16
  * bytes), heads and elements contiguous, dtype FADEMEM_F32 or FADEMEM_BF16.
@@ -420,7 +420,9 @@ int fademem_rope_apply(const fademem_rope* rope, int32_t dtype, const int32_t* p
  * The pool, the calls' buffers and the stream are used as fademem_cache uses
  * its own: one store is used by one host thread and one stream at a time (its
  * plan and its scratch too: two captured graphs of one store must not replay
- * at the same time).  Calls are made with the device current that was
+ * at the same time).  insert and attend belong to the plan before them; one that
+ * finds a plan of other `rows` or `max_new` on the device (a graph of them alone
+ * replayed after a different plan) does nothing.  Calls are made with the device current that was
  * current at creation (EINVAL otherwise).  FADEMEM_SERIALIZE works as above. */
 typedef struct fademem_paged_config {
   int32_t seqs;          /* sequences, 1..1024                                  */
@@ -433,7 +435,7 @@ typedef struct fademem_paged_config {
   int32_t sinks;         /* S >= 0, first blocks that stay visible             */
   int64_t pages;         /* pages of the pool, 1..2^24                         */
   int64_t max_tokens;    /* tokens of one sequence at most, 1..2^30            */
-  int64_t max_rows;      /* rows of one step at most, 1..2^24                  */
+  int64_t max_rows;      /* rows of one step at most, 1..2^23                  */
   int64_t block_tokens;  /* B, 1..2^30                                         */
   int64_t window;        /* blocks; 0: everything held is visible              */
   int32_t grid_h;        /* token p's position is (p / (grid_h * grid_w),      */
@@ -481,7 +483,8 @@ int fademem_paged_plan(fademem_paged* paged, const int32_t* kept, const int32_t*
  * Errors: EINVAL (NULL, unknown array, layer out of range). */
 enum {
   FADEMEM_PAGED_Q_START = 0,   /* int32 [seqs + 1]: first row of each sequence */
-  FADEMEM_PAGED_SLOTS = 1,     /* int64 [max_rows]: page * P + offset, or -1   */
+  FADEMEM_PAGED_SLOTS = 1,     /* int64 [max_rows]: page * P + offset, or -1;
+                                  the step's rows are written               */
   FADEMEM_PAGED_POSITIONS = 2, /* int32 [max_rows][3], 0 where the slot is -1  */
   FADEMEM_PAGED_STATUS = 3,    /* int32 [seqs]                                 */
   FADEMEM_PAGED_HELD = 4,      /* int32 [seqs]: tokens held, with the new ones */

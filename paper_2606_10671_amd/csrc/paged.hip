@@ -137,7 +137,7 @@ bool valid_config(const fademem_paged_config* c) {
   if (c->head_dim != 64 && c->head_dim != 128) return false;
   if (c->dtype != FADEMEM_F32 && c->dtype != FADEMEM_BF16) return false;
   if (c->page_tokens < 1 || c->page_tokens > 65536 || c->pages < 1 || c->pages > (int64_t(1) << 24)) return false;
-  if (c->max_tokens < 1 || c->max_tokens > most || c->max_rows < 1 || c->max_rows > (int64_t(1) << 24)) return false;
+  if (c->max_tokens < 1 || c->max_tokens > most || c->max_rows < 1 || c->max_rows > (int64_t(1) << 23)) return false;
   if (c->max_rows * (c->heads / c->kv_heads) > most || max_tiles(*c) * c->kv_heads > most) return false;
   if (c->block_tokens < 1 || c->block_tokens > most || c->window < 0 || c->window > most) return false;
   if (c->sinks < 0) return false;
@@ -153,7 +153,7 @@ __global__ void paged_init_kernel(PagedView v, int64_t words, int64_t entries) {
   const int64_t step = int64_t(gridDim.x) * blockDim.x, i0 = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
   if (i0 == 0) {
     v.header->free = int32_t(v.n_pages);
-    v.header->groups = v.header->tiles = v.header->refused = 0;
+    v.header->groups = v.header->tiles = v.header->refused = v.header->rows = v.header->max_new = 0;
     v.q_start[v.seqs] = 0;
   }
   for (int64_t i = i0; i < v.seqs; i += step) {
@@ -533,6 +533,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
     v.header->groups = launched;
     v.header->tiles = int32_t(n_tiles);
     v.header->refused = refused;
+    v.header->rows = int32_t(a.rows);
+    v.header->max_new = int32_t(a.max_new);
     v.header->even = e;
   }
   __syncthreads();
@@ -577,6 +579,7 @@ struct PagedInsertArgs {
   char* pages;              // of the layer
   size_t page_bytes;
   int64_t n_slots;          // pages * page_tokens
+  const PagedHeader* header;
   const int64_t* slots;
   const int32_t* pos;
   int64_t rows;
@@ -592,6 +595,7 @@ template <bool BF16, bool HALVES>
 __global__ __launch_bounds__(kRotThreads) void paged_insert_kernel(PagedInsertArgs a) {
   extern __shared__ __attribute__((aligned(16))) double2 cs[];
   constexpr int kElts = BF16 ? 8 : 4;
+  if (a.header->rows != a.rows) return;  // another step is planned
   const int64_t row0 = int64_t(blockIdx.x) * a.per_block;
   const int n = int(min(int64_t(a.per_block), a.rows - row0));
   if (a.rot.pairs > 0) {
@@ -769,6 +773,7 @@ int fademem_paged_insert(fademem_paged* c, int32_t layer, const void* k, int64_t
   a.pages = c->view.pages + size_t(layer) * c->view.layer_bytes;
   a.page_bytes = c->view.page_bytes;
   a.n_slots = c->cfg.pages * c->cfg.page_tokens;
+  a.header = c->view.header;
   a.slots = c->view.slots;
   a.pos = c->view.pos;
   a.rows = c->rows;
@@ -808,10 +813,11 @@ int fademem_paged_attend(fademem_paged* c, int32_t layer, const void* q, int64_t
   a.q_pitch = size_t(q_stride) * elt;
   a.out_pitch = size_t(out_stride) * elt;
   a.rows = c->rows;
+  a.max_new = c->max_new;
   a.scale = scale == 0.0f ? 1.0f / sqrtf(float(c->cfg.head_dim)) : scale;
   const bool bf16 = c->cfg.dtype == FADEMEM_BF16, narrow = narrow_step(c);
   hipError_t e = bf16 ? launch_paged_bf16(a, narrow, as_stream(stream)) : launch_paged_f32(a, narrow, as_stream(stream));
-  if (e == hipSuccess) e = launch_paged_finish(a, bf16, step_shape(c), c->max_new, as_stream(stream));
+  if (e == hipSuccess) e = launch_paged_finish(a, bf16, step_shape(c), as_stream(stream));
   if (e != hipSuccess) return hip_fail(c, e);
   return finish(c, stream);
 }

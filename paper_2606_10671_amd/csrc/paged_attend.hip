@@ -133,8 +133,9 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
   const CONST_AS int32_t* start = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
   const int groups = h[0], tiles = h[1], refused = h[2], join = plan_array(v.joins)[g];
   const int start_task = start[0];
-  const EvenPlan even = {h[3], h[4], h[5], h[6], h[7], h[8], h[9], h[10], h[11]};
+  const EvenPlan even = {h[5], h[6], h[7], h[8], h[9], h[10], h[11], h[12], h[13]};
   const bool is_even = shape.even && even.even;
+  if (h[3] != a.rows || h[4] != a.max_new) return;  // another step is planned
   // Parts: group g - 1's last units, then the first units of groups g, g + 1, ...; of an even plan, those of tile g
   // of the tiles left over.
   int parts = 0;
@@ -306,8 +307,8 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
 
 }  // namespace
 
-hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, int64_t max_new, hipStream_t stream) {
-  const int64_t most = max_new * a.v.group;  // rows of a sequence
+hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, hipStream_t stream) {
+  const int64_t most = a.max_new * a.v.group;  // rows of a sequence
   const int rows_used = int(most < 1 ? 1 : most < shape.rows ? most : shape.rows);
   // Narrow tiles: a block per row or, from five rows on, per four (32 rows of 32 tiles over 8000 tokens: a block per
   // row 104 us a call, per four 64); wide ones: a block per 32.

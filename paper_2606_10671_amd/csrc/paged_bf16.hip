@@ -100,7 +100,7 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
   __shared__ float m_s[kNarrowWaves][32], l_s[kNarrowWaves][32];
   __shared__ SegmentList segments;
   const PagedView& v = a.v;
-  const int groups = plan_array(&v.header->groups)[0];
+  const int groups = planned_groups(a);
   if (int(blockIdx.x) >= groups) return;
   const int g = xcd_group(blockIdx.x, groups);
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
@@ -334,7 +334,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
   char* const vbuf[3] = {v_lds0, v_lds1, v_lds2};
   __shared__ SegmentList segments;
   const PagedView& v = a.v;
-  const int groups = plan_array(&v.header->groups)[0];
+  const int groups = planned_groups(a);
   if (int(blockIdx.x) >= groups) return;
   const int g = xcd_group(blockIdx.x, groups);
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;

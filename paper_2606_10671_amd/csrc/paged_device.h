@@ -47,6 +47,12 @@ struct Segment {
   TileSpan span;
 };
 
+// Workgroups with work; none if the plan on the device is another step's.
+__device__ __forceinline__ int planned_groups(const PagedAttendArgs& a) {
+  const CONST_AS int32_t* h = plan_array(&a.v.header->groups);
+  return h[3] == a.rows && h[4] == a.max_new ? h[0] : 0;
+}
+
 // What follows from a segment's task.
 __device__ __forceinline__ void describe(const PagedView& v, TileShape shape, Segment& s) {
   s.seq = plan_array(v.tile_seq)[s.task / v.kv_heads];  // a sequence's tasks are kv_heads times its tiles, as is their first

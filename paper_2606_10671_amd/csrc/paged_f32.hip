@@ -126,7 +126,7 @@ __device__ __forceinline__ void paged_narrow_f32_body(const PagedAttendArgs& a) 
   __shared__ float m_s[kNarrowWaves][32], l_s[kNarrowWaves][32];
   __shared__ SegmentList segments;
   const PagedView& v = a.v;
-  const int groups = plan_array(&v.header->groups)[0];
+  const int groups = planned_groups(a);
   if (int(blockIdx.x) >= groups) return;
   const int g = xcd_group(blockIdx.x, groups);
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
@@ -305,7 +305,7 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
   __shared__ __attribute__((aligned(16))) float v_lds1[kObj];
   __shared__ SegmentList segments;
   const PagedView& v = a.v;
-  const int groups = plan_array(&v.header->groups)[0];
+  const int groups = planned_groups(a);
   if (int(blockIdx.x) >= groups) return;
   const int g = xcd_group(blockIdx.x, groups);
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;

@@ -116,7 +116,7 @@ int fademem_rope_apply(const fademem_rope* rope, int32_t dtype, const int32_t* p
   RopeArgs a;
   if (int rc = rotary_arg(rope, inverse, &a.rot)) return rc;
   if (dtype != FADEMEM_F32 && dtype != FADEMEM_BF16) return FADEMEM_EINVAL;
-  if (rows < 0 || rows > (int64_t(1) << 30) || heads < 1 || heads > 4096) return FADEMEM_EINVAL;
+  if (rows < 0 || rows > (int64_t(1) << 23) || heads < 1 || heads > 4096) return FADEMEM_EINVAL;
   const int elt = dtype == FADEMEM_BF16 ? 2 : 4;
   const int64_t row = int64_t(heads) * rope->head_dim;
   for (int64_t s : {x_stride, y_stride})
@@ -134,7 +134,6 @@ int fademem_rope_apply(const fademem_rope* rope, int32_t dtype, const int32_t* p
   a.heads = heads;
   a.per_block = rows_per_block(rows, int(row * elt / 16), a.rot.pairs);
   const int64_t blocks = (rows + a.per_block - 1) / a.per_block;
-  if (blocks > int64_t(0x7fffffff)) return FADEMEM_EINVAL;
   const bool bf16 = dtype == FADEMEM_BF16, halves = a.rot.halves != 0;
   auto kernel = bf16 ? (halves ? rope_kernel<true, true> : rope_kernel<true, false>)
                      : (halves ? rope_kernel<false, true> : rope_kernel<false, false>);

@@ -244,6 +244,156 @@ def test_values_that_a_row_does_not_see_do_not_reach_it(dtype, bad):
     p.attend()
 
 
+# -- larger ones, against fp64 on the GPU ---------------------------------------
+
+def large(dtype, D, heads, kv_heads, P, lens, news, block=1, window=0, sinks=0, pages=None, lse=True):
+    """One step of sequences that hold `lens` tokens and get `news`; the reference is torch in fp64, from the
+    same keys and values (bounds as in paged_parity: A, the weighted mean of |V|, carries the weights' error)."""
+    import torch
+    from paper_2606_10671_amd.paged import PagedCache
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    seqs, G = len(lens), heads // kv_heads
+    need = sum(-(-(a + b) // P) for a, b in zip(lens, news))
+    c = PagedCache(seqs=seqs, pages=pages or need + 3, page_tokens=P, heads=heads, kv_heads=kv_heads, head_dim=D, dtype=td,
+                   max_tokens=max(a + b for a, b in zip(lens, news)), max_rows=max(sum(lens), sum(news), 1), block_tokens=block,
+                   window=window, sinks=sinks)
+    c.pages().fill_(float("nan"))
+    torch.manual_seed(sum(lens) + D)
+    kv = [[torch.randn((a + b, kv_heads, D), device="cuda").to(td) for _ in range(2)] for a, b in zip(lens, news)]
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    if sum(lens):
+        c.plan(i32([0] * seqs), i32(lens), rows=sum(lens), max_new=max(lens))
+        c.insert(*(torch.cat([kv[s][w][:lens[s]] for s in range(seqs)]) for w in (0, 1)))
+    rows = sum(news)
+    c.plan(i32(lens), i32(news), rows=rows, max_new=max(news))
+    c.insert(*(torch.cat([kv[s][w][lens[s]:] for s in range(seqs)]) for w in (0, 1)))
+    assert c.status.tolist() == [0] * seqs
+    q = torch.randn((rows, heads, D), device="cuda").to(td)
+    L = torch.full((heads, rows), 7.0, device="cuda") if lse else None
+    out = c.attend(q, lse=L).double()
+    at = 0
+    for s in range(seqs):
+        n, held = news[s], lens[s] + news[s]
+        if n == 0:
+            continue
+        p, j = torch.arange(lens[s], held, device="cuda")[:, None] // block, torch.arange(held, device="cuda")[None] // block
+        seen = j <= p
+        if window:
+            seen &= (j > p - window) | (j < sinks)
+        k, v = (x.double().transpose(0, 1).repeat_interleave(G, 0).contiguous() for x in kv[s])  # [heads][held][D]
+        w = torch.matmul(q[at:at + n].double().transpose(0, 1).contiguous(), k.transpose(1, 2).contiguous()) / D ** 0.5
+        size = float(w.abs().max()) * D ** 0.5  # the products' sizes sum to at most the root of D times |q| |k| here
+        w = w.masked_fill(~seen, float("-inf"))
+        ref_l = torch.logsumexp(w, 2)
+        w = torch.softmax(w, 2)
+        ref, A = torch.matmul(w, v), torch.matmul(w, v.abs())
+        d = 2 * (D + 2) * 2.0**-24 * size
+        step = 2.0**-8 if dtype == "bf16" else 2.0**-24
+        tol = step * ref.abs() + ((2.0**-8 if dtype == "bf16" else 0.0) + 2 * d + (held + 16) * 2.0**-24) * A
+        err = (out[at:at + n].transpose(0, 1) - ref).abs()
+        assert bool((err <= tol).all()), (s, float((err - tol).max()))
+        if lse:
+            assert bool(((L[:, at:at + n].double() - ref_l).abs() <= d + (held + 16) * 2.0**-24 + 2.0**-22 * ref_l.abs()).all()), s
+        at += n
+    return c, q, out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_equal_tiles_are_dealt_evenly(dtype):
+    """More tiles than workgroups, and a few left over that are cut into parts and tails."""
+    say("even", dtype)
+    large(dtype, 64, 130, 130, 64, [900], [300], block=300)
+    large(dtype, 128, 50, 10, 64, [600, 600], [300, 300], block=300, window=2, sinks=1)
+    large(dtype, 128, 9, 9, 64, [2000], [1000], block=1000)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_unequal_tiles_share_workgroups(dtype):
+    say("uneven", dtype)
+    large(dtype, 64, 16, 4, 48, [0, 2000, 31, 700, 5, 0], [513, 100, 1, 300, 0, 65], window=600, sinks=4)
+    large(dtype, 128, 8, 1, 16, [3000, 10, 0], [40, 333, 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_tile_shared_by_every_workgroup(dtype):
+    say("long", dtype)
+    large(dtype, 128, 1, 1, 64, [70000], [1])
+    large(dtype, 64, 2, 1, 30, [40000], [150], block=1000)
+
+
+def test_more_segments_than_one_list_holds():
+    """A workgroup's segments are described 64 at a time: many short sequences and heads."""
+    say("many segments")
+    large("bf16", 64, 48, 48, 16, [3] * 500, [1] * 500)
+    large("bf16", 64, 40, 40, 16, [20] * 600, [40] * 599 + [41])
+
+
+def test_pages_beyond_32_bit_offsets():
+    """Sequences whose pages lie more than 2^32 bytes and 2^31 elements into the pool."""
+    say("far pages")
+    import torch
+    from paper_2606_10671_amd.paged import PagedCache
+    c = PagedCache(seqs=2, pages=24000, page_tokens=64, heads=8, kv_heads=8, head_dim=128, max_tokens=64 * 23990, max_rows=1 << 21)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    held = 0
+    while held < 64 * 23900:  # the first sequence takes the low pages
+        n = min(1 << 20, 64 * 23900 - held)
+        c.plan(i32([held, 0]), i32([n, 0]), rows=n, max_new=n)
+        held += n
+    k, v = (torch.randn((600, 8, 128), device="cuda").bfloat16() for _ in range(2))
+    c.plan(i32([held, 0]), i32([0, 600]), rows=600, max_new=600)
+    assert int(c.table[1, 0]) == 23900 and int(c.slots[0]) == 23900 * 64
+    c.insert(k, v)
+    assert torch.equal(c.pages()[23900, 0].transpose(0, 1), k[:64]) and torch.equal(c.pages()[23909, 1, :, 23], v[599])
+    q = torch.randn((600, 8, 128), device="cuda").bfloat16()
+    near = PagedCache(seqs=2, pages=20, page_tokens=64, heads=8, kv_heads=8, head_dim=128, max_tokens=1000, max_rows=1000)
+    near.plan(i32([0, 0]), i32([0, 600]), rows=600, max_new=600)
+    near.insert(k, v)
+    assert torch.equal(c.attend(q), near.attend(q))
+    for store, first in ((c, held), (near, 0)):
+        store.plan(i32([first, 600]), i32([0, 1]), rows=1, max_new=1)
+        store.insert(k[:1], v[:1])
+    assert torch.equal(c.attend(q[:1]), near.attend(q[:1]))
+
+
+def test_calls_of_another_step_do_nothing():
+    """A graph of insertion and attention alone, replayed after a plan with other rows or for another kernel."""
+    import torch
+    from paper_2606_10671_amd.paged import PagedCache
+    c = PagedCache(seqs=2, pages=60, page_tokens=16, heads=4, kv_heads=2, head_dim=64, max_tokens=400, max_rows=300)
+    c.pages().zero_()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn((100, h, 64), device="cuda").bfloat16() for h in (4, 2, 2))
+    out, lse = torch.zeros_like(q), torch.zeros((4, 100), device="cuda")
+
+    def calls():
+        c.insert(k, v)
+        c.attend(q, out=out, lse=lse)
+
+    c.plan(i32([0, 0]), i32([60, 40]), rows=100, max_new=60)
+    calls()
+    want = out.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for kept, new, rows, most in (([0, 0], [200, 100], 300, 200), ([0, 0], [1, 2], 100, 2), ([0, 0], [99, 1], 100, 99),
+                                  ([0, 0], [0, 0], 0, 0)):
+        c.plan(i32(kept), i32(new), rows=rows, max_new=most)
+        c.pages().zero_()
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert bool((out == 7.0).all()) and bool((lse == 7.0).all())
+        if rows != 100:
+            assert int(torch.count_nonzero(c.pages())) == 0
+    c.plan(i32([0, 0]), i32([60, 40]), rows=100, max_new=60)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
 # -- together --------------------------------------------------------------------
 
 def test_streams_generate_together():

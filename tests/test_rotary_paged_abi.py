@@ -32,7 +32,7 @@ GOOD = dict(dtype=BF16, pos_ptr=A, rows=8, heads=2, x_ptr=A, x_stride=128, y_ptr
 
 
 @pytest.mark.parametrize("change", [dict(dtype=2), dict(pos_ptr=0), dict(pos_ptr=A + 2), dict(rows=-1),
-                                    dict(rows=(1 << 30) + 1), dict(heads=0), dict(heads=5000), dict(x_ptr=0),
+                                    dict(rows=(1 << 23) + 1), dict(heads=0), dict(heads=5000), dict(x_ptr=0),
                                     dict(x_ptr=A + 8), dict(y_ptr=2 * A + 2), dict(y_ptr=0), dict(x_stride=127),
                                     dict(x_stride=132), dict(y_stride=120), dict(y_stride=-128), dict(inverse=2),
                                     dict(y_ptr=A + 128),                     # one row over another
@@ -76,7 +76,7 @@ def test_paged_bytes():
                                          ("heads", 0), ("kv_heads", 0), ("kv_heads", 3), ("head_dim", 96),
                                          ("dtype", 2), ("page_tokens", 0), ("page_tokens", 65537), ("pages", 0),
                                          ("pages", (1 << 24) + 1), ("max_tokens", 0), ("max_tokens", (1 << 30) + 1),
-                                         ("max_rows", 0), ("max_rows", (1 << 24) + 1), ("block_tokens", 0),
+                                         ("max_rows", 0), ("max_rows", (1 << 23) + 1), ("block_tokens", 0),
                                          ("block_tokens", (1 << 30) + 1), ("window", -1),
                                          ("window", (1 << 30) + 1), ("sinks", -1), ("grid_h", 0), ("grid_w", 0),
                                          ("grid_h", (1 << 30) + 1)])
@@ -95,7 +95,7 @@ def test_sizes_that_overflow_are_refused():
     big = {**CONFIG, "pages": 1 << 24, "page_tokens": 65536, "layers": 4096, "kv_heads": 4096, "heads": 4096}
     with pytest.raises(fm.FademError):
         fm.fademem_paged_bytes(fm.fademem_paged_config(**big))
-    rows = {**CONFIG, "max_rows": 1 << 24, "heads": 4096, "kv_heads": 1}
+    rows = {**CONFIG, "max_rows": 1 << 23, "heads": 4096, "kv_heads": 1}
     with pytest.raises(fm.FademError):
         fm.fademem_paged_bytes(fm.fademem_paged_config(**rows))
 
