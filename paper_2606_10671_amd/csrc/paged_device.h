@@ -177,7 +177,8 @@ __device__ __forceinline__ QueryRow query_row(const PagedView& v, const Segment&
   return q;
 }
 
-// Page numbers of a wave's next tiles of 32 keys, which begin at multiples of 32.
+// Page numbers of a wave's next tiles of 32 keys, which begin at multiples of 32 or
+// (a window's) of PagedView::align.
 // Lane j holds page j % n of tile batch + j / n, n pages at most lying under a
 // tile; a row's lane fetches its page's number from there.  A table read per tile
 // would have to be waited for behind the tile loads issued before it.

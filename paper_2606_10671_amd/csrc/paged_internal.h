@@ -109,6 +109,8 @@ struct PagedView {
   int32_t page_tokens, width;
   int32_t front;       // pages that hold sinks
   int32_t grid_h, grid_w;
+  int32_t align;       // a window's first tile begins at a multiple of this, a power of two that keeps it in the
+                       // page of its first key: 64 or 32 where pages are multiples of that, P where P divides 32, or 1
   uint32_t page_magic;  // key / page_tokens = key * page_magic >> page_shift for keys below 2^30
   int32_t page_shift;
 };
@@ -138,7 +140,7 @@ struct TileSpan {
 };
 __host__ __device__ inline TileSpan tile_span(const PagedView& v, int32_t p0, int32_t p1, int32_t held, int unit_keys) {
   TileSpan t;
-  const int32_t low = paged_low(v, p0) & ~63;  // pages of whole 64s are then read from a whole 64 on
+  const int32_t low = paged_low(v, p0) & ~(v.align - 1);
   t.end = paged_high(v, p1, held);
   const bool apart = v.sink_tokens < low;
   t.sinks = apart ? v.sink_tokens : 0;

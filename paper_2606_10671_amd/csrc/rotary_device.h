@@ -47,7 +47,7 @@ __device__ __forceinline__ void rotary_angles(const RotaryArg& r, const int32_t*
 // Eight fp64 values rounded once to bf16.  Rounding by way of fp32 is off only
 // where the fp32 value is a tie between two bf16 values and the fp64 one is not:
 // those few go through round-to-odd, which costs three times as much (a chunk of
-// 4680 rows of 12 x 128: 10.8 us with it everywhere, 8.0 so).
+// 4680 rows of 12 x 128: 10.8 us with it everywhere, 9.5 so).
 __device__ __forceinline__ void pack_unit(const double (&y)[8], rot_u32x4& out) {
   bool tie = false;
 #pragma unroll
