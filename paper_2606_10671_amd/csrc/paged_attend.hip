@@ -305,6 +305,16 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
   }
 }
 
+using FinishKernel = void (*)(PagedAttendArgs, TileShape, int);
+
+// The kernel whose blocks join `rows` rows.
+template <bool BF16, int D>
+FinishKernel finish_kernel(int rows) {
+  return rows == 32 ? paged_finish_kernel<BF16, D, false, 32, 2>
+         : rows == 1 ? paged_finish_kernel<BF16, D, true, 1, 4>
+                     : paged_finish_kernel<BF16, D, true, 4, 2>;
+}
+
 }  // namespace
 
 hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape shape, hipStream_t stream) {
@@ -314,14 +324,8 @@ hipError_t launch_paged_finish(const PagedAttendArgs& a, bool bf16, TileShape sh
   // row 104 us a call, per four 64); wide ones: a block per 32.
   const bool d128 = a.v.head_dim == 128, narrow = shape.rows == kPagedMinTileRows;
   const int rows = !narrow ? 32 : rows_used <= 4 ? 1 : 4;
-  void (*kernel)(PagedAttendArgs, TileShape, int);
-  if (d128) {
-    if (bf16) kernel = !narrow ? paged_finish_kernel<true, 128, false, 32, 2> : rows == 1 ? paged_finish_kernel<true, 128, true, 1, 4> : paged_finish_kernel<true, 128, true, 4, 2>;
-    else kernel = !narrow ? paged_finish_kernel<false, 128, false, 32, 2> : rows == 1 ? paged_finish_kernel<false, 128, true, 1, 4> : paged_finish_kernel<false, 128, true, 4, 2>;
-  } else {
-    if (bf16) kernel = !narrow ? paged_finish_kernel<true, 64, false, 32, 2> : rows == 1 ? paged_finish_kernel<true, 64, true, 1, 4> : paged_finish_kernel<true, 64, true, 4, 2>;
-    else kernel = !narrow ? paged_finish_kernel<false, 64, false, 32, 2> : rows == 1 ? paged_finish_kernel<false, 64, true, 1, 4> : paged_finish_kernel<false, 64, true, 4, 2>;
-  }
+  const FinishKernel kernel = bf16 ? (d128 ? finish_kernel<true, 128>(rows) : finish_kernel<true, 64>(rows))
+                                   : (d128 ? finish_kernel<false, 128>(rows) : finish_kernel<false, 64>(rows));
   hipLaunchKernelGGL(kernel, dim3(unsigned(shape.groups), unsigned((rows_used + rows - 1) / rows)), dim3(kFinishThreads), 0,
                      stream, a, shape, rows_used);
   return hipGetLastError();

@@ -16,7 +16,7 @@ from __future__ import annotations
 from typing import Optional, Tuple
 
 from . import fademem as fm
-from .rotary import Rotary, rows_of
+from .rotary import Rotary, empty_rows, rows_of
 
 
 class PagedCache:
@@ -107,7 +107,7 @@ class PagedCache:
         rows, heads, dim = self.rows, self._heads, self._dim
         q_stride = rows_of(q, "q", self.torch_dtype, self.device, heads, dim, rows)
         if out is None:
-            out, out_stride = torch.empty((rows, heads, dim), dtype=self.torch_dtype, device=self.device), heads * dim
+            out, out_stride = empty_rows((rows, heads, dim), self.torch_dtype, self.device, stream), heads * dim
         else:
             out_stride = rows_of(out, "out", self.torch_dtype, self.device, heads, dim, rows)
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != self.device

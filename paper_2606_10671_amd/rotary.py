@@ -23,6 +23,17 @@ def rows_of(t, name: str, dtype, device, heads: int, head_dim: int, rows: int) -
     return pitch if rows > 1 else heads * head_dim
 
 
+def empty_rows(shape, dtype, device, stream):
+    """Memory for the result of a call on `stream` (None: the current one),
+    taken from that stream's: what the current stream has let go it may still
+    be working on."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class Rotary:
     """A rotation: `pairs` = (time, height, width) pairs of a head, in this
     order from its first pair on (the rest is copied); pair k of an axis with
@@ -58,7 +69,7 @@ class Rotary:
         if pos.dtype != torch.int32 or pos.shape != (rows, 3) or not pos.is_contiguous() or pos.device != device:
             raise ValueError(f"pos: expected a contiguous int32 [{rows}][3] tensor on {device}")
         if out is None:
-            out, y_stride = torch.empty((rows, heads, self.head_dim), dtype=dtype, device=device), heads * self.head_dim
+            out, y_stride = empty_rows((rows, heads, self.head_dim), dtype, device, stream), heads * self.head_dim
         else:
             y_stride = rows_of(out, "out", dtype, device, heads, self.head_dim, rows)
         with fm.on_device(device.index):

@@ -476,6 +476,24 @@ def test_calls_repeat_bit_for_bit_on_another_stream():
     assert torch.equal(first, again)
 
 
+def test_a_result_on_another_stream_takes_no_memory_that_this_stream_let_go():
+    import torch
+    p = Pair(1, pages=100, P=64, heads=12, D=128, max_tokens=6000, max_rows=6000)
+    p.plan([0], [5000])
+    p.insert()
+    q = torch.randn((5000, 12, 128), device="cuda").bfloat16()
+    first = p.cache.attend(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    gone = torch.empty_like(q)  # work of the current stream may still read it
+    at = gone.data_ptr()
+    del gone
+    again = p.cache.attend(q, stream=side)
+    assert again.data_ptr() != at
+    side.synchronize()
+    assert torch.equal(first, again)
+
+
 def test_refusals():
     import torch
     from paper_2606_10671_amd import fademem as fm

@@ -141,6 +141,22 @@ def test_given_frequencies_and_streams():
     assert torch.equal(y[..., 20:], x[..., 20:])
 
 
+def test_a_result_on_another_stream_takes_no_memory_that_this_stream_let_go():
+    import torch
+    from paper_2606_10671_amd.rotary import Rotary
+    x = torch.randn((5000, 12, 64), device="cuda")
+    pos = torch.zeros((5000, 3), dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    gone = torch.empty_like(x)  # work of the current stream may still read it
+    at = gone.data_ptr()
+    del gone
+    y = Rotary(64, (32, 0, 0)).apply(x, pos, stream=side)
+    assert y.data_ptr() != at
+    side.synchronize()
+    assert torch.equal(x, y)
+
+
 def test_a_captured_call_replays_with_other_positions():
     import torch
     from paper_2606_10671_amd.rotary import Rotary
