@@ -114,7 +114,8 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, 
 
 // grid = (groups at most, chunks of a tile's rows): a block joins ROWS rows of the
 // tile that workgroup blockIdx.x is the first to begin inside.  Bound by latency:
-// kernel arguments, plan, partial results (beside the sequence's lengths), results.
+// kernel arguments, plan, partial results (beside the sequence's lengths), results;
+// 8 to 11 us, 16 to 18 where every workgroup shares a tile of 256 x 128.
 // SLICED = false (wide tiles, few parts): a thread takes four elements of several
 // rows, two parts at a time.  SLICED (narrow tiles, up to hundreds of parts): the
 // block's threads share out the parts of ROWS rows, AHEAD of them in flight per

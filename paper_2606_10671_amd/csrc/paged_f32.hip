@@ -8,7 +8,9 @@
 // and added to the running one; the queries carry only the scale's power of two,
 // the rest of it enters in the one rounding that takes a score's distance to the
 // row max.  Bound by the matrix cores (2 x 64 MFMAs of 64 cycles per block at
-// D = 128); narrow tiles of few rows by those too, or by reading K and V.
+// D = 128) and by the softmax between them, which on a SIMD does not run beside fp32
+// MFMAs: 2 x 1170 rows of 12 heads over 5850 keys, 84 GFLOP in 815 us, matrix cores busy 71% of the
+// cycles.  Narrow tiles of few rows by those too, or by reading K and V.
 #include "paged_device.h"
 
 namespace fademem {

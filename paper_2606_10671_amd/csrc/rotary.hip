@@ -4,7 +4,9 @@
 // A block takes a few rows: the angles' cos and sin of each (row, pair) are made
 // once, in LDS, and serve every head of the row; then every thread turns
 // 16-byte units (for half-split pairs: two of them).  Reads and writes each
-// element once.
+// element once.  Bound by memory where the call is large (fp32 10 007 rows of
+// 24 x 64: 123 MB in 20 us, 6.1 TB/s), below that by the chain of launch, angles and
+// one round of loads (bf16 4680 rows of 12 x 128: 28.8 MB in 9.5 us; 16 rows 3.6).
 #include <math.h>
 
 #include "rotary_device.h"
