@@ -77,7 +77,7 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   const unsigned __int128 page = (unsigned __int128)2 * unsigned(c.kv_heads) * uint64_t(P) * unsigned(c.head_dim) * elt;
   const unsigned __int128 layer = page * uint64_t(c.pages);
   if (page > (uint64_t(1) << 31) || layer * unsigned(c.layers) > kMaxPool || seqs * uint64_t(width) * 4 > kMaxPool) return false;
-  const TileShape wide = c.dtype == FADEMEM_BF16 ? kPagedWideBf16 : kPagedWideF32;
+  const TileShape wide = c.dtype == FADEMEM_BF16 ? paged_wide_bf16_shape(c.head_dim) : kPagedWideF32;
   const TileShape narrow = c.dtype == FADEMEM_BF16 ? kPagedNarrowBf16 : kPagedNarrowF32;
   v->pool = pool;
   v->header = reinterpret_cast<PagedHeader*>(take(sizeof(PagedHeader)));
@@ -644,7 +644,7 @@ __global__ __launch_bounds__(kRotThreads) void paged_insert_kernel(PagedInsertAr
 // would read the keys once for every 32 of them.
 bool narrow_step(const fademem_paged* c) { return c->max_new * c->view.group <= kPagedNarrowBf16.rows; }
 TileShape step_shape(const fademem_paged* c) {
-  return c->cfg.dtype == FADEMEM_BF16 ? (narrow_step(c) ? kPagedNarrowBf16 : kPagedWideBf16)
+  return c->cfg.dtype == FADEMEM_BF16 ? (narrow_step(c) ? kPagedNarrowBf16 : paged_wide_bf16_shape(c->cfg.head_dim))
                                       : (narrow_step(c) ? kPagedNarrowF32 : kPagedWideF32);
 }
 

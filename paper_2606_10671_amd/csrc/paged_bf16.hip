@@ -17,9 +17,6 @@
 namespace fademem {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWaves = kThreads / 64;
-
 template <int D>
 struct Row {
   static constexpr int CH = D / 8;         // 16-byte chunks
@@ -303,7 +300,8 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
 }
 
 // ---------------------------------------------------------------------------
-// Wide tiles: 256 rows, 8 waves x 32.  Bound by the matrix cores.  The pipeline
+// Wide tiles: 8 waves x 32 rows, or 4 at D = 64, where a CU has LDS for two such
+// workgroups.  Bound by the matrix cores.  The pipeline
 // is the one of the unpaged attention: K/V tiles of 64 keys go from the pages
 // straight into three-deep LDS rings, two tiles ahead, one barrier per tile;
 // iteration t runs S(t+1) = K(t+1) Q^T beside the exponentials of S(t)'s second
@@ -318,7 +316,7 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
 // product of two 8192 x 8192 matrices; 12 x 4680 rows over 23 400 keys 1.13, the matrix cores busy 61% of
 // the cycles.  Many short tasks are bound by what each costs beside its units, first
 // loads and last results (24 ragged sequences, 16 heads of 64 over 4: 28 GFLOP in
-// 69 us, matrix cores busy 24%).
+// 65 us).
 // ---------------------------------------------------------------------------
 
 constexpr float kRescaleBound = 256.0f;
@@ -328,6 +326,8 @@ constexpr int kKeys = 64;
 template <int D, bool WHOLE>
 __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
   using R = Row<D>;
+  constexpr TileShape kShape = paged_wide_bf16_shape(D);
+  constexpr int kWaves = kShape.rows / 32, kThreads = 64 * kWaves;
   constexpr int kTileBytes = kKeys * D * 2;
   constexpr int kLoads = kKeys * R::CH / kThreads;  // 16-byte loads per lane and tile, for K and for V
   __shared__ __attribute__((aligned(16))) char k_lds0[kTileBytes];
@@ -367,7 +367,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
     ld_voff[i] = uint32_t(ld_row(i) * D * 2) + ld_vch(i);
   }
 
-  for_segments(v, kPagedWideBf16, g, segments, [&](const Segment& s) {
+  for_segments(v, kShape, g, segments, [&](const Segment& s) {
     const CONST_AS int32_t* table = plan_array(v.table + size_t(s.seq) * v.width);
     const char* pages = a.pages + size_t(s.head) * P * D * 2;
     const int n_sink = s.span.n_sink, end = s.span.end, from = s.span.from, sinks = s.span.sinks;
@@ -424,6 +424,12 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
       if (t + 1 < s.u1) find(t + 1);
     };
 
+    // The wave's share of the task's eight bytes.
+    auto mark = [&](int bad) {
+      uint8_t* marks = reinterpret_cast<uint8_t*>(v.redo + s.task);
+      marks[wave] = uint8_t(bad);
+      if constexpr (kWaves == 4) marks[4 + wave] = 0;
+    };
     // A wave without rows (a sequence's last tile is usually partial) only
     // issues its share of the loads and meets the barriers.
     if (wave * 32 >= s.rows) {
@@ -441,7 +447,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
           load_tile(t + 2, b == 0 ? kbuf[0] : b == 1 ? kbuf[1] : kbuf[2], b == 0 ? vbuf[0] : b == 1 ? vbuf[1] : vbuf[2]);
         b = b == 2 ? 0 : b + 1;
       }
-      if (s.u0 == 0 && lane == 0) reinterpret_cast<uint8_t*>(v.redo + s.task)[wave] = 0;
+      if (s.u0 == 0 && lane == 0) mark(0);
       return;
     }
 
@@ -685,9 +691,9 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
         }
       if (a.lse && hh == 0 && r < s.rows) a.lse[size_t(qr.head) * a.rows + qr.row] = (m * c2 + __log2f(l)) * kLn2;
       const bool bad = __any(r < s.rows && !(__builtin_fabsf(all) < INFINITY));
-      if (lane == 0) reinterpret_cast<uint8_t*>(v.redo + s.task)[wave] = bad ? 1 : 0;
+      if (lane == 0) mark(bad ? 1 : 0);
     } else {
-      float* slot = v.scratch + size_t(max(s.slot, 0)) * paged_slot_floats(kPagedWideBf16.rows, D);
+      float* slot = v.scratch + size_t(max(s.slot, 0)) * paged_slot_floats(kShape.rows, D);
       if (r < s.rows) {
         float* row = slot + size_t(r) * D + 4 * hh;
 #pragma unroll
@@ -697,11 +703,11 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
             *reinterpret_cast<float4*>(row + 32 * db + 8 * g4) =
                 make_float4(o[db][4 * g4], o[db][4 * g4 + 1], o[db][4 * g4 + 2], o[db][4 * g4 + 3]);
         if (hh == 0) {
-          slot[256 * D + r] = m * c2;
-          slot[256 * (D + 1) + r] = l;
+          slot[kShape.rows * D + r] = m * c2;
+          slot[kShape.rows * (D + 1) + r] = l;
         }
       }
-      if (s.u0 == 0 && lane == 0) reinterpret_cast<uint8_t*>(v.redo + s.task)[wave] = 0;
+      if (s.u0 == 0 && lane == 0) mark(0);
     }
   });
 }
@@ -711,7 +717,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void paged_narrow_bf16(PagedAtte
   paged_narrow_body<D>(a);
 }
 template <int D, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 1) void paged_wide_bf16(PagedAttendArgs a) {
+__global__ __launch_bounds__(2 * paged_wide_bf16_shape(D).rows, 2 - paged_wide_bf16_shape(D).rows / 256) void paged_wide_bf16(PagedAttendArgs a) {
   paged_wide_body<D, WHOLE>(a);
 }
 
@@ -719,11 +725,12 @@ __global__ __launch_bounds__(kThreads, 1) void paged_wide_bf16(PagedAttendArgs a
 
 hipError_t launch_paged_bf16(const PagedAttendArgs& a, bool narrow, hipStream_t stream) {
   const bool d128 = a.v.head_dim == 128, whole = a.v.page_tokens % kKeys == 0;
+  const TileShape wide = paged_wide_bf16_shape(a.v.head_dim);
   auto kernel = narrow ? (d128 ? paged_narrow_bf16<128> : paged_narrow_bf16<64>)
                 : whole ? (d128 ? paged_wide_bf16<128, true> : paged_wide_bf16<64, true>)
                         : (d128 ? paged_wide_bf16<128, false> : paged_wide_bf16<64, false>);
-  hipLaunchKernelGGL(kernel, dim3(unsigned(narrow ? kPagedNarrowBf16.groups : kPagedWideBf16.groups)),
-                     dim3(narrow ? kNarrowThreads : kThreads), 0, stream, a);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(narrow ? kPagedNarrowBf16.groups : wide.groups)),
+                     dim3(narrow ? kNarrowThreads : 2 * wide.rows), 0, stream, a);
   return hipGetLastError();
 }
 

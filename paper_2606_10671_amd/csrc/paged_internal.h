@@ -39,8 +39,15 @@ struct TileShape {
 // (Overheads of 2, 4, 6, 8 of the wide bf16 kernel: 24 ragged sequences 85.0, 76.0,
 // 74.9, 73.7 us, one chunk of 12 heads x 4680 rows 648, 640, 636, 627 us.  Least
 // parts of 1, 2, 4 units of the narrow one: 5 sequences x 32 heads over up to 5000
-// tokens 16.2, 18.0, 20.6 us.)
+// tokens 16.2, 18.0, 20.6 us.  At D = 64 two workgroups of 128 rows share a CU, one
+// computing while the other begins or ends a task: 24 ragged sequences 80 us with
+// 256 rows, 76 so, 64 short ones 60 and 50, 32 whole prompts of 1024 tokens 160 and
+// 148, one long chunk 1057 and 1070; overheads of 2, 4, 6, 8 there 83, 76, 78, 80.)
 constexpr TileShape kPagedWideBf16 = {256, 64, 256, 8, 6, 1};
+constexpr TileShape kPagedWideBf16D64 = {128, 64, 512, 4, 6, 1};
+__host__ __device__ constexpr TileShape paged_wide_bf16_shape(int head_dim) {
+  return head_dim == 64 ? kPagedWideBf16D64 : kPagedWideBf16;
+}
 constexpr TileShape kPagedNarrowBf16 = {32, 128, 512, 1, 1, 0};
 constexpr TileShape kPagedWideF32 = {128, 64, 256, 1, 2, 1};
 constexpr TileShape kPagedNarrowF32 = {32, 128, 256, 1, 1, 0};
