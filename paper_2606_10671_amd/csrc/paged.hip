@@ -121,7 +121,7 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   // 2^(30+L) / P rounded up, 2^L >= P: the product is off by less than key / 2^(30+L) < 1/P.
   int shift = 30;
   while ((int64_t(1) << (shift - 30)) < P) ++shift;
-  v->page_shift = shift;
+  v->page_shift = shift - 30;
   v->page_magic = uint32_t(((uint64_t(1) << shift) + uint64_t(P) - 1) / uint64_t(P));
   v->grid_h = c.grid_h;
   v->grid_w = c.grid_w;

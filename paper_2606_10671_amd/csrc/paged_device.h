@@ -20,7 +20,7 @@ __device__ __forceinline__ const CONST_AS T* plan_array(const T* p) {
 }
 
 __device__ __forceinline__ int32_t safe_page(const PagedView& v, int32_t id) {
-  return min(max(id, 0), int32_t(v.n_pages) - 1);
+  return int32_t(min(uint32_t(id), uint32_t(v.n_pages) - 1u));
 }
 
 // Waits until at most N of the wave's loads are in flight (they land in order),
