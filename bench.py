@@ -56,14 +56,14 @@ FP32_MFMA_PEAK_TFLOPS = 157.3  # dense fp32 matrix-core peak
 # split tiles) at the wan1.3b-1layer workload, from rocprofv3 FETCH_SIZE and
 # WRITE_SIZE (see profiles/perf_cases.md), valid only for the
 # kernel source they were taken on (first 16 hex digits of its sha256).
-ATTN_TRAFFIC = {"source_sha256": "b1f732980ef42d52", "workload": "wan1.3b-1layer", "bytes_per_call": 966115584}
+ATTN_TRAFFIC = {"source_sha256": "3c80d54da8717880", "workload": "wan1.3b-1layer", "bytes_per_call": 965315392}
 
 
 # HBM bytes of one fused chunk update's data pass (update_data_kernel) in
 # the 30-layer update leg, from rocprofv3 FETCH_SIZE and WRITE_SIZE scaled
 # by the insert copy (see profiles/perf_cases.md); valid
 # only for the cache.hip source they were taken on.
-UPD_TRAFFIC = {"source_sha256": "90913cfbf3c0ac10", "workload": "wan1.3b-30layer-update", "bytes_per_call": 4259831160}
+UPD_TRAFFIC = {"source_sha256": "2ff1ef94ed36a1ad", "workload": "wan1.3b-30layer-update", "bytes_per_call": 4259809688}
 
 # HBM bytes of one spectral analysis call (all its kernels) at spectral-374clips, from rocprofv3 FETCH_SIZE and
 # WRITE_SIZE scaled by the insert copy (see profiles/perf_cases.md); valid only for this source.
