@@ -169,6 +169,51 @@ def test_rows_at_tile_edges(dtype, rows):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window", [0, 77])
+@pytest.mark.parametrize("P", [1, 3, 5, 8, 24, 31, 33, 96, 100, 300])
+def test_page_sizes(dtype, D, window, P):
+    """Tiles that begin and end anywhere in a page, one page under a tile or thirty-two: prompts, a chunk, single tokens."""
+    say("pages", dtype, D, window, P)
+    p = Pair(3, pages=3 * (-(-330 // P) + 2), P=P, heads=4, kv_heads=2, D=D, dtype=dtype, max_tokens=400, max_rows=500,
+             window=window, sinks=5 if window else 0)
+    for kept, new in (([0, 0, 0], [201, 70, 1]), ([201, 70, 1], [40, 97, 130]), ([241, 167, 131], [3, 1, 16]),
+                      ([244, 168, 147], [1, 1, 0])):
+        p.plan(kept, new)
+        p.insert()
+        p.attend()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,heads,kv_heads", [(64, 96, 1), (128, 40, 1), (64, 33, 1), (128, 66, 2)])
+def test_more_heads_than_a_narrow_tile(dtype, D, heads, kv_heads):
+    """One token's heads of a key head fill a wide tile, or more than one."""
+    say("heads", dtype, D, heads, kv_heads)
+    p = Pair(3, pages=60, P=32, heads=heads, kv_heads=kv_heads, D=D, dtype=dtype, max_tokens=700, max_rows=800)
+    p.plan([0, 0, 0], [1, 130, 500])
+    p.insert()
+    p.plan([1, 130, 500], [1, 1, 1])
+    p.insert()
+    p.attend()
+    p.plan([2, 131, 501], [7, 0, 4])
+    p.insert()
+    p.attend()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_as_many_sequences_as_there_may_be(dtype):
+    """1024 sequences that begin with one token: each sees itself."""
+    say("1024", dtype)
+    p = Pair(1024, pages=2048, P=16, heads=2, D=64, dtype=dtype, max_tokens=64, max_rows=4096)
+    p.plan([0] * 1024, [1] * 1024)
+    p.insert()
+    p.attend()
+    p.plan([1] * 1024, [i % 3 for i in range(1024)])
+    p.insert()
+    p.attend()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_long_memory_is_split(dtype):
     """Few rows over many keys: the keys are shared out among workgroups and joined."""
     say("long", dtype)
