@@ -353,22 +353,31 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
     auto issue = [&](int u, float* kb, float* vb) {
       const int key0 = key0_of(u), lim = lim_of(u);
       if (key0 < lim) {
+        int chunk = lane % R::CH;
+        // Offsets worked out anew for each unit: kept, they spill at D = 128 (24 ragged sequences 620 us, so 573; at
+        // D = 64, where they fit, one chunk of 16 heads 1582 us kept and 1608 anew).
+        if constexpr (D == 128) asm volatile("" : "+v"(chunk));
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-          const int c = ((i * kQW + qw) * 64 + lane) % R::CH, row = ld_row(i), key = min(key0 + row, lim - 1);
+          const int row = ld_row(i), key = min(key0 + row, lim - 1);
           const char* src = pages + size_t(uint32_t(safe_page(v, id[i]))) * v.page_bytes +
                             uint32_t(key - page_of(v, key) * P) * uint32_t(D * 4);
-          __builtin_amdgcn_global_load_lds(src + (c ^ (row & 15)) * 16,
+          __builtin_amdgcn_global_load_lds(src + (chunk ^ (row & 15)) * 16,
                                            (LDS_AS void*)(kb + split * R::TILE + (i * kQW + qw) * 256), 16, 0, 0);
-          __builtin_amdgcn_global_load_lds(src + v_off + c * 16,
+          __builtin_amdgcn_global_load_lds(src + v_off + chunk * 16,
                                            (LDS_AS void*)(vb + split * R::TILE + (i * kQW + qw) * 256), 16, 0, 0);
         }
       }
       if (u + 1 < s.u1) find(u + 1);
     };
-    auto compute = [&](int u, const float* kb, const float* vb) {
+    // Unit u, and the loads of the next one: at its start in split 0, behind the scores in split 1, so that of two
+    // waves on a SIMD one has products for the matrix cores while the other works out addresses (one chunk of 24 heads
+    // 15.85 ms with all loads at the start, 15.37 so; at D = 64 8.39, 8.15).
+    auto compute = [&](int u, const float* kb, const float* vb, float* kb_next, float* vb_next) {
       const int key0 = key0_of(u), lim = lim_of(u);
-      if (key0 >= lim || !active) return;
+      const bool more = u + 1 < s.u1, work = key0 < lim && active;
+      if (more && (split == 0 || !work)) issue(u + 1, kb_next, vb_next);
+      if (!work) return;
       const int e = key0 + kTile, high = min(qr.high, lim);
       const bool hides = !(e <= lim && e <= all_high && (key0 >= all_low || e <= v.sink_tokens));
       tile_f32<D>(
@@ -377,7 +386,10 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
             const int key = key0 + j;
             return !(key < high && (key >= qr.low || key < v.sink_tokens));
           },
-          [] {}, [] {}, m, l, o);
+          [&] {
+            if (more && split > 0) issue(u + 1, kb_next, vb_next);
+          },
+          [] {}, m, l, o);
     };
 
     __syncthreads();  // the last segment's reads are done
@@ -386,13 +398,11 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
     for (int u = s.u0; u < s.u1; u += 2) {
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();  // unit u's tiles landed for every wave; the other buffers are free
-      if (u + 1 < s.u1) issue(u + 1, k_lds1, v_lds1);
-      compute(u, k_lds0, v_lds0);
+      compute(u, k_lds0, v_lds0, k_lds1, v_lds1);
       if (u + 1 >= s.u1) break;
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
-      if (u + 2 < s.u1) issue(u + 2, k_lds0, v_lds0);
-      compute(u + 1, k_lds1, v_lds1);
+      compute(u + 1, k_lds1, v_lds1, k_lds0, v_lds0);
     }
 
     // Join the splits: split 1 leaves its registers, one object per wave.
