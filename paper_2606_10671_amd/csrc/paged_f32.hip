@@ -81,9 +81,10 @@ __device__ __forceinline__ void tile_f32(const f32x4 (&q)[D / 8], const float* k
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     s[r] = __builtin_fmaf(s[r], rest, -m_ref);
-    least = fminf(least, s[r] == -INFINITY ? 0.0f : s[r]);
+    least = fminf(least, s[r]);
   }
-  // The instruction alone makes weights below 2^-126 zero, exp2f does not.
+  // The instruction alone makes weights below 2^-126 zero, exp2f does not.  (Tiles with a hidden key take exp2f too:
+  // to tell them apart would cost every tile two instructions a score.)
   if (__any(least < -126.0f)) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = exp2f(s[r]);
