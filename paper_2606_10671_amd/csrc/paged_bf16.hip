@@ -316,7 +316,7 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
 // product of two 8192 x 8192 matrices; 12 x 4680 rows over 23 400 keys 1.13, the matrix cores busy 61% of
 // the cycles.  Many short tasks are bound by what each costs beside its units, first
 // loads and last results (24 ragged sequences, 16 heads of 64 over 4: 28 GFLOP in
-// 65 us).
+// 62 us).
 // ---------------------------------------------------------------------------
 
 constexpr float kRescaleBound = 256.0f;

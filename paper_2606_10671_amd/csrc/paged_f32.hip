@@ -9,7 +9,7 @@
 // the rest of it enters in the one rounding that takes a score's distance to the
 // row max.  Bound by the matrix cores (2 x 64 MFMAs of 64 cycles per block at
 // D = 128) and by the softmax between them, which on a SIMD does not run beside fp32
-// MFMAs: 2 x 1170 rows of 12 heads over 5850 keys, 84 GFLOP in 815 us, matrix cores busy 71% of the
+// MFMAs: 2 x 1170 rows of 12 heads over 5850 keys, 84 GFLOP in 775 us, matrix cores busy 74% of the
 // cycles.  Narrow tiles of few rows by those too, or by reading K and V.
 #include "paged_device.h"
 
