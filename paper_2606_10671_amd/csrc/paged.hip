@@ -263,36 +263,6 @@ __device__ __forceinline__ void write_row(const PagedView& v, int64_t i, bool li
   v.pos[3 * i + 2] = x;
 }
 
-// The even dealing of `total` tiles of `units` key units (EvenPlan); returns the
-// workgroups with work.  Head parts: as many as the groups allow, none shorter
-// than the shape's least.  Tails for the groups left over: a tail costs its
-// group the overhead of a tile again, counted as half of shape.overhead beyond a
-// head part's own; tails that take less than two units off every head part are
-// left out.
-constexpr int kMinTailSaves = 2;
-__device__ int even_plan(int total, int units, TileShape shape, EvenPlan* e) {
-  e->even = 1;
-  e->groups = shape.groups;
-  e->units = units;
-  e->rounds = total / shape.groups;
-  e->rem = total - e->rounds * shape.groups;
-  e->heads = e->tails_per = 1;
-  e->tail_len = 0;
-  if (e->rem > 0) {
-    e->heads = max(1, min(shape.groups / e->rem, units / shape.min_part));
-    const int left = shape.groups - e->heads * e->rem;
-    if (left > 0 && units >= shape.min_part) {
-      e->tails_per = (e->rem + left - 1) / left;
-      const int over = (shape.overhead + 1) / 2 * (e->tails_per - 1) * e->heads;
-      const int len = units > over ? (units - over) / (e->tails_per * e->heads + 1) : 0;
-      if (len >= kMinTailSaves * e->heads) e->tail_len = len;
-    }
-  }
-  e->head_len = units - e->tail_len;
-  if (e->rounds > 0) return shape.groups;
-  return e->heads * e->rem + (e->tail_len > 0 ? (e->rem + e->tails_per - 1) / e->tails_per : 0);
-}
-
 // The step's plan, one block: thread s has sequence s.  What each sequence gives
 // back and needs follows from its lengths alone; prefix sums over the sequences
 // say where its rows, pages and row tiles begin.  Pages are bits of a map, so

@@ -53,6 +53,12 @@ __device__ __forceinline__ int planned_groups(const PagedAttendArgs& a) {
   return h[3] == a.rows && h[4] == a.max_new ? h[0] : 0;
 }
 
+// How the plan deals equal tiles.
+__device__ __forceinline__ EvenPlan planned_even(const PagedView& v) {
+  const CONST_AS int32_t* e = plan_array(&v.header->even.even);
+  return {e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7], e[8]};
+}
+
 // What follows from a segment's task.
 __device__ __forceinline__ void describe(const PagedView& v, TileShape shape, Segment& s) {
   s.seq = plan_array(v.tile_seq)[s.task / v.kv_heads];  // a sequence's tasks are kv_heads times its tiles, as is their first
@@ -77,11 +83,8 @@ struct SegmentList {
 
 // Segments of workgroup g.
 __device__ __forceinline__ int count_segments(const PagedView& v, TileShape shape, int g) {
-  const CONST_AS int32_t* e = plan_array(&v.header->even.even);
-  if (shape.even && e[0]) {
-    const int rounds = e[2], rem = e[3], heads = e[4], tail_len = e[6], tails_per = e[7], i0 = (g - heads * rem) * tails_per;
-    return rounds + (g < heads * rem ? 1 : tail_len > 0 && i0 < rem ? min(tails_per, rem - i0) : 0);
-  }
+  const EvenPlan e = planned_even(v);
+  if (shape.even && e.even) return even_segments(e, g);
   const CONST_AS int32_t* w = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
   return w[2] - w[0] + (w[3] > 0 && (w[2] > w[0] || w[3] > w[1]) ? 1 : 0);
 }
@@ -92,27 +95,16 @@ __device__ __forceinline__ void list_segments(const PagedView& v, TileShape shap
   const int i = int(threadIdx.x), k = first + i;
   if (i >= kSegBatch || k >= n) return;
   Segment s;
-  const CONST_AS int32_t* e = plan_array(&v.header->even.even);
-  s.u0 = 0;
-  s.slot = -1;
-  if (shape.even && e[0]) {
-    const int groups = e[1], rounds = e[2], rem = e[3], heads = e[4], head_len = e[5], tail_len = e[6];
-    const int base = rounds * groups, head_groups = heads * rem;
-    s.task = k * groups + g;
-    s.u1 = e[8];
-    if (k >= rounds && g < head_groups) {
-      const int j = g / rem;
-      s.task = base + g - j * rem;
-      s.u0 = j * head_len / heads;
-      s.u1 = (j + 1) * head_len / heads;
-      if (heads > 1 || tail_len > 0) s.slot = g;
-    } else if (k >= rounds) {
-      s.task = base + (g - head_groups) * e[7] + k - rounds;
-      s.u0 = head_len;
-      s.slot = head_groups + s.task - base;
-    }
+  const EvenPlan e = planned_even(v);
+  if (shape.even && e.even) {
+    const EvenSegment x = even_segment(e, g, k);
+    s.task = x.task;
+    s.u0 = x.u0;
+    s.u1 = x.u1;
+    s.slot = x.slot;
     describe(v, shape, s);
   } else {
+    s.u0 = 0;
     const CONST_AS int32_t* w = plan_array(reinterpret_cast<const int32_t*>(v.starts + g));
     s.task = w[0] + k;
     describe(v, shape, s);

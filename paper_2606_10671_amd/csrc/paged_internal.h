@@ -73,6 +73,69 @@ struct EvenPlan {
   int32_t units;      // of a tile
 };
 
+// The even dealing of `total` tiles of `units` key units (EvenPlan); returns the
+// workgroups with work.  Head parts: as many as the groups allow, none shorter
+// than the shape's least.  Tails for the groups left over: a tail costs its
+// group the overhead of a tile again, counted as half of shape.overhead beyond a
+// head part's own; tails that take less than two units off every head part are
+// left out.
+constexpr int kMinTailSaves = 2;
+__host__ __device__ inline int even_plan(int total, int units, TileShape shape, EvenPlan* e) {
+  e->even = 1;
+  e->groups = shape.groups;
+  e->units = units;
+  e->rounds = total / shape.groups;
+  e->rem = total - e->rounds * shape.groups;
+  e->heads = e->tails_per = 1;
+  e->tail_len = 0;
+  if (e->rem > 0) {
+    const int most = shape.groups / e->rem, long_enough = units / shape.min_part, heads = most < long_enough ? most : long_enough;
+    e->heads = heads > 1 ? heads : 1;
+    const int left = shape.groups - e->heads * e->rem;
+    if (left > 0 && units >= shape.min_part) {
+      e->tails_per = (e->rem + left - 1) / left;
+      const int over = (shape.overhead + 1) / 2 * (e->tails_per - 1) * e->heads;
+      const int len = units > over ? (units - over) / (e->tails_per * e->heads + 1) : 0;
+      if (len >= kMinTailSaves * e->heads) e->tail_len = len;
+    }
+  }
+  e->head_len = units - e->tail_len;
+  if (e->rounds > 0) return shape.groups;
+  return e->heads * e->rem + (e->tail_len > 0 ? (e->rem + e->tails_per - 1) / e->tails_per : 0);
+}
+
+// Unit at which part j of the first `len` units begins, cut into `parts`: j * len / parts, whose product passes 32 bits
+// from 2^31 / parts units on (one tile over 2^28 keys at 512 workgroups).
+__host__ __device__ inline int32_t even_cut(int32_t len, int32_t parts, int32_t j) {
+  const int32_t q = len / parts;
+  return j * q + j * (len - q * parts) / parts;
+}
+
+// Segments of workgroup g, and the k-th of them: task, units, slot of its partial result or -1.
+struct EvenSegment {
+  int32_t task, u0, u1, slot;
+};
+__host__ __device__ inline int32_t even_segments(const EvenPlan& e, int32_t g) {
+  const int32_t i0 = (g - e.heads * e.rem) * e.tails_per, left = e.rem - i0;
+  return e.rounds + (g < e.heads * e.rem ? 1 : e.tail_len > 0 && left > 0 ? (left < e.tails_per ? left : e.tails_per) : 0);
+}
+__host__ __device__ inline EvenSegment even_segment(const EvenPlan& e, int32_t g, int32_t k) {
+  const int32_t base = e.rounds * e.groups, head_groups = e.heads * e.rem;
+  EvenSegment s = {k * e.groups + g, 0, e.units, -1};
+  if (k >= e.rounds && g < head_groups) {
+    const int32_t j = g / e.rem;
+    s.task = base + g - j * e.rem;
+    s.u0 = even_cut(e.head_len, e.heads, j);
+    s.u1 = even_cut(e.head_len, e.heads, j + 1);
+    if (e.heads > 1 || e.tail_len > 0) s.slot = g;
+  } else if (k >= e.rounds) {
+    s.task = base + (g - head_groups) * e.tails_per + k - e.rounds;
+    s.u0 = e.head_len;
+    s.slot = head_groups + s.task - base;
+  }
+  return s;
+}
+
 struct PagedHeader {
   int32_t free;    // free pages
   int32_t groups;  // workgroups with work (attention)
