@@ -553,7 +553,7 @@ struct PagedInsertArgs {
   const PagedHeader* header;
   const int64_t* slots;
   const int32_t* pos;
-  int64_t rows;
+  int64_t rows, max_new;    // of the step
   int kv_heads, head_dim, page_tokens;
   int per_block;            // rows of a block
   RotaryArg rot;            // pairs = 0: keys as they are
@@ -567,7 +567,7 @@ template <bool BF16, bool HALVES>
 __global__ __launch_bounds__(kRotThreads) void paged_insert_kernel(PagedInsertArgs a) {
   extern __shared__ __attribute__((aligned(16))) double2 cs[];
   constexpr int kElts = BF16 ? 8 : 4;
-  if (a.header->rows != a.rows) return;  // another step is planned
+  if (a.header->rows != a.rows || a.header->max_new != a.max_new) return;  // another step is planned
   const int64_t row0 = int64_t(blockIdx.x) * a.per_block;
   const int n = int(min(int64_t(a.per_block), a.rows - row0));
   if (a.rot.pairs > 0) {
@@ -753,6 +753,7 @@ int fademem_paged_insert(fademem_paged* c, int32_t layer, const void* k, int64_t
   a.slots = c->view.slots;
   a.pos = c->view.pos;
   a.rows = c->rows;
+  a.max_new = c->max_new;
   a.kv_heads = c->cfg.kv_heads;
   a.head_dim = c->cfg.head_dim;
   a.page_tokens = c->cfg.page_tokens;
