@@ -154,7 +154,7 @@ __global__ void paged_init_kernel(PagedView v, int64_t words, int64_t entries) {
   const int64_t step = int64_t(gridDim.x) * blockDim.x, i0 = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
   if (i0 == 0) {
     v.header->free = int32_t(v.n_pages);
-    v.header->groups = v.header->tiles = v.header->refused = v.header->rows = v.header->max_new = 0;
+    v.header->groups = v.header->tiles = v.header->refused = v.header->rows = v.header->max_new = v.header->again = 0;
     v.q_start[v.seqs] = 0;
   }
   for (int64_t i = i0; i < v.seqs; i += step) {
@@ -507,6 +507,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs a) {
     v.header->rows = int32_t(a.rows);
     v.header->max_new = int32_t(a.max_new);
     v.header->even = e;
+    v.header->again = 0;
   }
   __syncthreads();
   // Workgroup g is the first that begins inside its tile: the tile has parts from g - 1 on.

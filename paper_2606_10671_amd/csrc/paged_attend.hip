@@ -53,16 +53,18 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, 
   const int32_t* table = v.table + size_t(s) * v.width;
   const int sinks = min(v.sink_tokens, min(qr.low, qr.high));
   const float c2 = a.scale * kLog2e;
+  const char* const v0 = a.pages;
   float m = -INFINITY, l = 0.0f, o[kPer] = {};
+  bool dead = false;
   for (int part = 0; part < 2; ++part) {
     const int end = part ? qr.high : sinks;
     for (int k0 = part ? qr.low : 0; k0 < end; k0 += 64) {
       const int key = k0 + lane, n = min(64, end - k0);
-      const char* vrow = nullptr;
+      uint64_t v_at = 0;
       float x = -INFINITY;
       if (key < end) {
         const char* krow = key_row(a, table, key, hk, D * kElt);
-        vrow = krow + size_t(v.kv_heads) * v.page_tokens * D * kElt;
+        v_at = uint64_t(krow - v0) + size_t(v.kv_heads) * v.page_tokens * D * kElt;
         x = 0.0f;
         for (int d = 0; d < D; d += 16 / kElt) {
           const uint4 w = *reinterpret_cast<const uint4*>(krow + d * kElt);
@@ -87,9 +89,11 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, 
       l = l * alpha + wave_sum(p);
 #pragma unroll
       for (int e = 0; e < kPer; ++e) o[e] *= alpha;
-      for (int j = 0; j < n; ++j) {
-        const float pj = __shfl(p, j);
-        const char* vr = reinterpret_cast<const char*>(__shfl(reinterpret_cast<unsigned long long>(vrow), j));
+      // A key at a time for all of V's elements, eight of them in flight.
+      auto add = [&](int j) {
+        const float pj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), j));
+        const char* vr = v0 + ((uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(v_at >> 32), j))) << 32) |
+                               uint32_t(__builtin_amdgcn_readlane(uint32_t(v_at), j)));
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
           const int d = lane * kPer + e;
@@ -97,10 +101,23 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, 
                                 : reinterpret_cast<const float*>(vr)[d];
           o[e] = __builtin_fmaf(pj, x1, o[e]);
         }
+      };
+      if (!dead) {
+        int j = 0;
+        for (; j + 8 <= n; j += 8) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) add(j + i);
+        }
+        for (; j < n; ++j) add(j);
+        bool nan = true;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) nan = nan && o[e] != o[e];
+        dead = __all(nan);  // every element is NaN and stays it
       }
+      if (dead && !a.lse) break;
       if (l != l) break;  // a NaN score: every element is NaN
     }
-    if (l != l) break;
+    if (l != l || (dead && !a.lse)) break;
   }
   char* out = a.out + size_t(qr.row) * a.out_pitch + size_t(qr.head) * D * kElt;
 #pragma unroll
@@ -145,8 +162,11 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
   } else if (g > 0 && g < groups) {
     parts = join;
   }
-  const int64_t jobs = blockIdx.y == 0 ? int64_t(tiles) * v.kv_heads : 0;
-  uint64_t mark = int64_t(g) * kFinishThreads + tid < jobs ? v.redo[int64_t(g) * kFinishThreads + tid] : 0;
+  // Blocks of 32 rows of whole tiles, none if no attention since the plan marked any: thread t of block b looks at
+  // number b, and t times as many as there are blocks behind it, so that marked ones lying together go to different blocks.
+  const int per_shift = shape.rows == 32 ? 0 : shape.rows == 128 ? 2 : 3;  // 32-row blocks of a tile
+  const int64_t jobs = h[14] ? (int64_t(tiles) * v.kv_heads) << per_shift : 0, blocks = int64_t(gridDim.x) * gridDim.y;
+  const int64_t job0 = int64_t(blockIdx.y) * gridDim.x + g;
   Segment mine = {};
   bool again = false;
   if (parts > 1) {
@@ -260,11 +280,15 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
     mine = s;
   }
 
-  // Rows again: this block's, if joining them gave something that is not finite,
-  // and rows of whole tiles that the attention marked.
-  for (int64_t j0 = int64_t(g) * kFinishThreads; again || j0 < jobs; j0 += int64_t(gridDim.x) * kFinishThreads) {
-    if (j0 > int64_t(g) * kFinishThreads) mark = j0 + tid < jobs ? v.redo[j0 + tid] : 0;
-    if (!__syncthreads_or(mark != 0) && !again) continue;
+  // Rows again: this block's, if joining them gave something that is not finite, and rows of whole tiles that the
+  // attention marked.  An infinity or NaN that every row sees marks them all, and key by key a row costs 130 times
+  // what it does by matrix (4680 rows of 12 heads over 23 400 keys: 86 ms), so they are spread over all blocks: 512
+  // tiles of 128 rows over 640 keys 1.7 ms, 895 with 256 tiles to a block.
+  for (int64_t j0 = job0; again || j0 < jobs; j0 += blocks * kFinishThreads) {
+    const int64_t at = j0 + tid * blocks;
+    const int mark =
+        at < jobs ? reinterpret_cast<const uint8_t*>(v.redo)[(at >> per_shift) * 8 + (at & ((1 << per_shift) - 1))] : 0;
+    if (!__syncthreads_or(mark) && !again) continue;
     if (tid == 0) {
       n_list = again;
       list[0] = -1;
@@ -275,16 +299,14 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
     for (int i = 0; i < n_list; ++i) {
       Segment s = mine;
       int r0 = blockIdx.y * ROWS, r1 = min(r0 + ROWS, mine.rows);
-      uint64_t marks = ~uint64_t(0);
       if (list[i] >= 0) {
-        s.task = int(j0) + list[i];
+        const int64_t job = j0 + list[i] * blocks;
+        s.task = int(job >> per_shift);
         describe(v, shape, s);
-        r0 = 0;
-        r1 = s.rows;
-        marks = v.redo[s.task];
+        r0 = 32 * int(job & ((1 << per_shift) - 1));
+        r1 = min(r0 + 32, s.rows);
       }
-      for (int r = r0 + wave; r < r1; r += kFinishWaves)
-        if ((marks >> (8 * (r >> 5))) & 0xff) attend_row<BF16, D>(a, s.seq, query_row(v, s, r), q_s[wave]);
+      for (int r = r0 + wave; r < r1; r += kFinishWaves) attend_row<BF16, D>(a, s.seq, query_row(v, s, r), q_s[wave]);
     }
     again = false;
     __syncthreads();

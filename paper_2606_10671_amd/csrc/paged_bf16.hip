@@ -295,7 +295,10 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
       }
     }
     bad = __syncthreads_or(bad);
-    if (s.u0 == 0 && tid == 0) v.redo[s.task] = whole && bad ? ~uint64_t(0) : 0;
+    if (s.u0 == 0 && tid == 0) {
+      v.redo[s.task] = whole && bad ? ~uint64_t(0) : 0;
+      if (whole && bad) v.header->again = 1;
+    }
   });
 }
 
@@ -428,6 +431,7 @@ __device__ __forceinline__ void paged_wide_body(const PagedAttendArgs& a) {
     auto mark = [&](int bad) {
       uint8_t* marks = reinterpret_cast<uint8_t*>(v.redo + s.task);
       marks[wave] = uint8_t(bad);
+      if (bad) v.header->again = 1;
       if constexpr (kWaves == 4) marks[4 + wave] = 0;
     };
     // A wave without rows (a sequence's last tile is usually partial) only

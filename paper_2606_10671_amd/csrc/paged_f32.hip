@@ -282,7 +282,10 @@ __device__ __forceinline__ void paged_narrow_f32_body(const PagedAttendArgs& a) 
       }
     }
     bad = __syncthreads_or(bad);
-    if (s.u0 == 0 && tid == 0) v.redo[s.task] = whole && bad ? ~uint64_t(0) : 0;
+    if (s.u0 == 0 && tid == 0) {
+      v.redo[s.task] = whole && bad ? ~uint64_t(0) : 0;
+      if (whole && bad) v.header->again = 1;
+    }
   });
 }
 
@@ -460,7 +463,10 @@ __device__ __forceinline__ void paged_wide_f32_body(const PagedAttendArgs& a) {
         if (a.lse && hh == 0) a.lse[size_t(qr.head) * a.rows + qr.row] = (m + log2f(l)) * kLn2;
       }
       const bool bad = __any(r < s.rows && !(__builtin_fabsf(all) < INFINITY));
-      if (lane == 0) redo[qw] = bad ? 1 : 0;
+      if (lane == 0) {
+        redo[qw] = bad ? 1 : 0;
+        if (bad) v.header->again = 1;
+      }
     } else {
       float* slot = v.scratch + size_t(max(s.slot, 0)) * paged_slot_floats(kPagedWideF32.rows, D);
       if (r < s.rows) {

@@ -144,6 +144,7 @@ struct PagedHeader {
   int32_t rows;    // rows and most new tokens that the step was planned with: a call
   int32_t max_new; // made for others (a replayed graph's, say) does nothing
   EvenPlan even;
+  int32_t again;   // 1: since the plan, some attention marked rows that are to be worked out again (PagedView::redo)
 };
 
 // The store as kernels see it.
