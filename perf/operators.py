@@ -60,7 +60,7 @@ def listed():
         # The gradient through the rotation at narrow heads, an odd number of rows inside a joint projection, the
         # half-split pairing, part of each head left as it is.
         _rope("rope-grad-d64-f32", "f32", 10007, 24, 64, (8, 10, 10), "halves", inverse=True, fused=True, grid=(37, 41)),
-        # One more token of 256 sequences: the tables of a decoding step.
+        # One more token of 256 sequences, the last one rejected: the tables of a decoding step that goes back and on.
         _paged("plan-decode", "plan", "bf16", 8, 8, 128, 16, 256, (50, 4000), (1, 1)),
         # Eight streams leave and eight start with their first chunk: many pages, many rows.
         _paged("plan-wave", "plan", "bf16", 12, 12, 128, 64, 8, (4680, 4680), (4680, 4680), block=4680, window=4,
@@ -491,8 +491,8 @@ def run(state):
         if not own:
             return _plan_plain(st)
         cache = st["cache"]
-        if c["wave"]:
-            cache.plan(st["zero"], st["zero"], rows=0, max_new=0)
+        # Back to before the step (a step planned again changes nothing, so it would deal out no page), then the step.
+        cache.plan(st["zero"] if c["wave"] else st["kept"], st["zero"], rows=0, max_new=0)
         cache.plan(st["zero"] if c["wave"] else st["kept"], st["new"], rows=st["rows"], max_new=st["most"])
         n = st["rows"]
         return dict(q_start=cache.q_start, slots=cache.slots[:n], pos=cache.pos[:n], table=cache.table, held=cache.held,
