@@ -165,3 +165,20 @@ def test_one_value_that_every_row_sees_does_not_stall_the_call(dtype):
     print("again", dtype, a.elapsed_time(b), "ms", flush=True)
     assert bool(torch.isposinf(out[..., 3]).all()) and bool(torch.isfinite(out[..., 4:]).all())
     assert a.elapsed_time(b) < 50.0
+
+
+def test_going_back_and_on_deals_the_same_pages():
+    """A step planned again changes nothing; gone back from and planned again, it gives its pages back and gets the same."""
+    import torch
+    from paper_2606_10671_amd.paged import PagedCache
+    c = PagedCache(seqs=5, pages=80, page_tokens=4, heads=2, head_dim=64, max_tokens=100, max_rows=200, window=20, sinks=2)
+    kept, new, zero = i32([40, 33, 7, 0, 16]), i32([1, 9, 1, 30, 0]), i32([0] * 5)
+    c.plan(zero, kept, rows=200, max_new=40)
+    c.plan(kept, new, rows=41, max_new=30)
+    want = [x.clone() for x in (c.table, c.slots[:41], c.pos[:41], c.held, c.status, c.free)]
+    for back in (False, True, True):
+        if back:
+            c.plan(kept, zero, rows=0, max_new=0)
+            assert c.held.tolist() == kept.tolist() and int(c.free[0]) > int(want[5][0])
+        c.plan(kept, new, rows=41, max_new=30)
+        assert all(torch.equal(a, b) for a, b in zip(want, (c.table, c.slots[:41], c.pos[:41], c.held, c.status, c.free)))
