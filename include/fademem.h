@@ -358,7 +358,9 @@ int fademem_spectral_fit(const double* t, const double* r, int64_t n, int32_t it
  * caller applies to a chunk's queries and keys.  With fademem_config's
  * rope_pairs the memory turns its own keys by their entry index (Sec. 3.3
  * "Boundary and positional handling"); the time axis here is the same
- * rotation (same pairs, same frequencies, same bits).
+ * rotation, by the same pairs and frequencies.  Both are evaluated in fp64, by
+ * code of their own: an element of one may be the neighbour of the other's
+ * where the fp64 value lies next to the border of a rounding.
  * Pair p of a head turns by the angle pos[row][axis of p] * freq[p]:
  * (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos), evaluated in fp64 and
  * rounded once to the storage type.  The first pairs[0] pairs follow axis 0
