@@ -29,7 +29,8 @@ class PagedCache:
     (int32 [seqs+1]), ``slots`` (int64 [max_rows]), ``pos`` (int32
     [max_rows][3]), ``status`` and ``held`` (int32 [seqs]), ``table`` (int32
     [seqs][pages of max_tokens]) and ``free`` (int32 [1]) are views of the
-    step's plan on the device.
+    step's plan on the device.  The store is for inference: no gradient passes
+    through insert and attend.
     """
 
     def __init__(self, seqs: int, pages: int, page_tokens: int, heads: int, head_dim: int,

@@ -5,6 +5,8 @@ of a chunk's queries and keys, and its inverse, which is its gradient.
 """
 from __future__ import annotations
 
+import contextlib
+import functools
 from typing import Optional, Sequence
 
 from . import fademem as fm
@@ -34,6 +36,29 @@ def empty_rows(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+@functools.lru_cache(maxsize=None)
+def _turn():
+    """Rotary.apply as a step of torch's autograd (made on first use: the package imports torch only in calls)."""
+    import torch
+
+    class Turn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, pos, rotary, inverse):
+            pos = pos.clone()  # a step's positions are written over by the next plan
+            ctx.save_for_backward(pos)
+            ctx.rotary, ctx.inverse = rotary, inverse
+            return rotary.apply(x, pos, inverse=inverse)
+
+        @staticmethod
+        def backward(ctx, g):
+            pos, = ctx.saved_tensors
+            g = g.contiguous()
+            g = g if g.data_ptr() % 16 == 0 else g.clone()
+            return ctx.rotary.apply(g, pos, inverse=not ctx.inverse), None, None, None
+
+    return Turn
+
+
 class Rotary:
     """A rotation: `pairs` = (time, height, width) pairs of a head, in this
     order from its first pair on (the rest is copied); pair k of an axis with
@@ -59,7 +84,8 @@ class Rotary:
         """x [rows][heads][head_dim] (float32 or bfloat16; rows may be apart,
         as in a joint projection's output) turned to the positions pos, a
         contiguous int32 [rows][3] tensor of (time, height, width).  out may be
-        x.  inverse=True turns back: the gradient of apply."""
+        x.  inverse=True turns back: the gradient of apply, which autograd takes
+        by itself where x wants one (not into a given `out`)."""
         import torch
         dtype, device = x.dtype, x.device
         if (dtype != torch.bfloat16 and dtype != torch.float32) or x.dim() != 3 or not x.is_cuda:
@@ -68,6 +94,11 @@ class Rotary:
         x_stride = rows_of(x, "x", dtype, device, heads, self.head_dim, rows)
         if pos.dtype != torch.int32 or pos.shape != (rows, 3) or not pos.is_contiguous() or pos.device != device:
             raise ValueError(f"pos: expected a contiguous int32 [{rows}][3] tensor on {device}")
+        if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
+            if out is not None:
+                raise ValueError("out: a result that takes part in autograd cannot be written into given memory")
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):  # the gradient's stream too
+                return _turn().apply(x, pos, self, inverse)
         if out is None:
             out, y_stride = empty_rows((rows, heads, self.head_dim), dtype, device, stream), heads * self.head_dim
         else:
