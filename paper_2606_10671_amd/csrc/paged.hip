@@ -118,11 +118,7 @@ bool lay_out(const fademem_paged_config& c, char* pool, PagedView* v, size_t* to
   v->width = int32_t(width);
   v->front = int32_t((v->sink_tokens + P - 1) / P);
   v->align = P % 64 == 0 ? 64 : P % 32 == 0 ? 32 : 32 % P == 0 ? int32_t(P) : 1;
-  // 2^(30+L) / P rounded up, 2^L >= P: the product is off by less than key / 2^(30+L) < 1/P.
-  int shift = 30;
-  while ((int64_t(1) << (shift - 30)) < P) ++shift;
-  v->page_shift = shift - 30;
-  v->page_magic = uint32_t(((uint64_t(1) << shift) + uint64_t(P) - 1) / uint64_t(P));
+  set_page_division(v, P);
   v->grid_h = c.grid_h;
   v->grid_w = c.grid_w;
   if (at > kMaxPool) return false;

@@ -182,13 +182,21 @@ struct PagedView {
   int32_t grid_h, grid_w;
   int32_t align;       // a window's first tile begins at a multiple of this, a power of two that keeps it in the
                        // page of its first key: 64 or 32 where pages are multiples of that, P where P divides 32, or 1
-  uint32_t page_magic;  // key / page_tokens = (key * page_magic >> 30) >> page_shift for keys below 2^30
+  uint32_t page_magic;  // key / page_tokens = (key * page_magic >> 31) >> page_shift for keys below 2^31
   int32_t page_shift;
 };
 
-// Page of a token (below 2^30).
+// 2^(31+L) / P rounded up, 2^L >= P: the product is off by less than key / 2^(31+L) < 1/P.
+inline void set_page_division(PagedView* v, int64_t P) {
+  int shift = 31;
+  while ((int64_t(1) << (shift - 31)) < P) ++shift;
+  v->page_shift = shift - 31;
+  v->page_magic = uint32_t(((uint64_t(1) << shift) + uint64_t(P) - 1) / uint64_t(P));
+}
+
+// Page of a token (or of a sequence's end, 2^30 at most).
 __host__ __device__ inline int32_t page_of(const PagedView& v, int32_t key) {
-  return int32_t(uint32_t((uint64_t(uint32_t(key) << 2) * v.page_magic) >> 32) >> v.page_shift);
+  return int32_t(uint32_t((uint64_t(uint32_t(key) << 1) * v.page_magic) >> 32) >> v.page_shift);
 }
 
 // First key of the window of a query at position p, and the end of what it sees.

@@ -52,3 +52,34 @@ def test_a_sequence_of_more_than_two_to_the_28_tokens():
         assert bool(((out[:new[0]] - want).abs() <= want * (2.0**-8 + 2.0**-12)).all()), (out[0, :4], want[0, :4])
         assert bool(((lse[0, :new[0]].double() - n.log()).abs() <= 2.0**-12 + 2.0**-22 * math.log(base)).all())
         assert bool((out[new[0]:, [0, 3]] == 1.0).all()) and bool((out[new[0]:, 1:3] == 0.0).all())
+
+
+def test_a_sequence_of_two_to_the_30_tokens():
+    """Through a window of one block: its last tokens are attended as in a short sequence, it may be planned at its very
+    end, where the window has left every page behind, and starts again."""
+    import torch
+    from paper_2606_10671_amd.paged import PagedCache
+    end, P, D, n = 1 << 30, 65536, 64, 70
+    c = PagedCache(seqs=1, pages=2 * (1 << 23) // P + 3, page_tokens=P, heads=2, kv_heads=1, head_dim=D, max_tokens=end,
+                   max_rows=1 << 23, block_tokens=P, window=1)
+    near = PagedCache(seqs=1, pages=3, page_tokens=P, heads=2, kv_heads=1, head_dim=D, max_tokens=P, max_rows=P,
+                      block_tokens=P, window=1)
+    for held in range(0, end, 1 << 23):
+        c.plan(i32([held]), i32([1 << 23]), rows=1 << 23, max_new=1 << 23)
+    assert c.status.tolist() == [0] and c.held.tolist() == [end]
+    near.plan(i32([0]), i32([P]), rows=P, max_new=P)
+    c.pages().zero_()
+    near.pages().zero_()
+    q, k, v = (torch.randn((n, h, D), device="cuda").bfloat16() for h in (2, 1, 1))
+    c.plan(i32([end - n]), i32([n]), rows=n, max_new=n)
+    near.plan(i32([P - n]), i32([n]), rows=n, max_new=n)
+    assert c.status.tolist() == [0] and c.pos[:n, 0].tolist() == list(range(end - n, end))
+    for store in (c, near):
+        store.insert(k, v)
+    assert torch.equal(c.attend(q), near.attend(q))
+    c.plan(i32([end]), i32([0]), rows=0, max_new=0)
+    assert c.status.tolist() == [0] and c.held.tolist() == [end] and int(c.free[0]) == 2 * (1 << 23) // P + 3
+    c.plan(i32([end]), i32([1]), rows=1, max_new=1)
+    assert c.status.tolist() == [-1]
+    c.plan(i32([0]), i32([5]), rows=5, max_new=5)
+    assert c.status.tolist() == [0] and c.slots[:5].tolist() == [0, 1, 2, 3, 4]

@@ -1,6 +1,6 @@
 """Arithmetic of the paged memory that host and device share, compiled for the
-host from the library's own header: the dealing of equal tiles to workgroups, at
-every length that the header allows."""
+host from the library's own header: the dealing of equal tiles to workgroups and
+the pages of tokens, at every length that the header allows."""
 import ctypes
 import os
 import subprocess
@@ -13,6 +13,11 @@ SOURCE = r"""
 #include "paged_internal.h"
 using namespace fademem;
 extern "C" {
+int page(int P, int key) {
+  PagedView v;
+  set_page_division(&v, P);
+  return page_of(v, key);
+}
 int cut(int len, int parts, int j) { return even_cut(len, parts, j); }
 // The segments of a plan of `total` tiles of `units` units, workgroup by workgroup: (task, u0, u1, slot) each.
 // Returns their number, or -1 beyond `most`.
@@ -44,6 +49,18 @@ def lib(tmp_path_factory):
                     "-I", os.path.join(build.ROOT, "include"), "-I", os.path.join(build.PKG, "csrc"), str(src), "-o", str(out)],
                    check=True, timeout=300)
     return ctypes.CDLL(str(out))
+
+
+@pytest.mark.parametrize("P", [1, 2, 3, 5, 7, 16, 31, 33, 48, 63, 64, 100, 127, 129, 300, 1000, 4680, 32767, 32769, 65535, 65536])
+def test_pages_of_tokens(lib, P):
+    """Around every kind of multiple up to the longest sequence, whose end (2^30) is asked for too."""
+    keys = {0, 1, 2, (1 << 30) - 1, 1 << 30}
+    for base in (0, 1 << 10, 1 << 20, 1 << 24, 1 << 28, 1 << 29, (1 << 30) - 3 * P):
+        for k in range(4):
+            m = (base // P + k) * P
+            keys |= {m - 1, m, m + 1, m + P // 2}
+    for key in sorted(k for k in keys if 0 <= k <= 1 << 30):
+        assert lib.page(P, key) == key // P, key
 
 
 UNITS = [1, 5, 6, 7, 74, 383, 9143, (1 << 22) - 1, 1 << 22, (1 << 22) + 1, (1 << 23) + 5, (1 << 24) - 1, (1 << 24) + 1]
