@@ -437,7 +437,9 @@ typedef struct fademem_paged_config {
   int32_t sinks;         /* S >= 0, first blocks that stay visible             */
   int64_t pages;         /* pages of the pool, 1..2^24                         */
   int64_t max_tokens;    /* tokens of one sequence at most, 1..2^30            */
-  int64_t max_rows;      /* rows of one step at most, 1..2^23                  */
+  int64_t max_rows;      /* rows of one step at most, 1..2^23; with G = heads /
+                            kv_heads, max_rows * G and (max_rows * G / 32 +
+                            seqs) * kv_heads are at most 2^30                  */
   int64_t block_tokens;  /* B, 1..2^30                                         */
   int64_t window;        /* blocks; 0: everything held is visible              */
   int32_t grid_h;        /* token p's position is (p / (grid_h * grid_w),      */

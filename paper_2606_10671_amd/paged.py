@@ -43,8 +43,9 @@ class PagedCache:
         if dtype not in (torch.float32, torch.bfloat16):
             raise ValueError("dtype must be torch.float32 or torch.bfloat16")
         kv_heads = heads if kv_heads is None else kv_heads
-        max_tokens = pages * page_tokens if max_tokens is None else max_tokens
-        max_rows = max_tokens if max_rows is None else max_rows
+        # Left open: all that the pages hold, and a step of as much, up to what the library takes.
+        max_tokens = min(pages * page_tokens, 1 << 30) if max_tokens is None else max_tokens
+        max_rows = min(max_tokens, 1 << 23, (1 << 30) // max(1, heads // max(1, kv_heads))) if max_rows is None else max_rows
         self.torch_dtype = dtype
         self.cfg = fm.fademem_paged_config(
             seqs=seqs, layers=layers, heads=heads, kv_heads=kv_heads, head_dim=head_dim,

@@ -182,3 +182,17 @@ def test_going_back_and_on_deals_the_same_pages():
             assert c.held.tolist() == kept.tolist() and int(c.free[0]) > int(want[5][0])
         c.plan(kept, new, rows=41, max_new=30)
         assert all(torch.equal(a, b) for a, b in zip(want, (c.table, c.slots[:41], c.pos[:41], c.held, c.status, c.free)))
+
+
+def test_a_store_of_more_tokens_than_a_step_may_have():
+    """Without max_tokens and max_rows: all that the pages hold, in steps of the most rows that the library takes."""
+    import torch
+    from paper_2606_10671_amd.paged import PagedCache
+    c = PagedCache(seqs=1, pages=1 << 18, page_tokens=64, heads=1, head_dim=64)
+    assert c.cfg.max_tokens == 1 << 24 and c.cfg.max_rows == 1 << 23
+    c.plan(i32([0]), i32([1 << 23]), rows=1 << 23, max_new=1 << 23)
+    c.plan(i32([1 << 23]), i32([1 << 23]), rows=1 << 23, max_new=1 << 23)
+    assert c.status.tolist() == [0] and c.held.tolist() == [1 << 24] and int(c.free[0]) == 0
+    assert torch.equal(c.slots, torch.arange(1 << 23, 1 << 24, device="cuda"))
+    c = PagedCache(seqs=1, pages=1 << 16, page_tokens=64, heads=1024, kv_heads=1, head_dim=64)
+    assert c.cfg.max_rows == 1 << 20
