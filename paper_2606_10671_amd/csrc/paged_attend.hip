@@ -89,7 +89,7 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, 
       l = l * alpha + wave_sum(p);
 #pragma unroll
       for (int e = 0; e < kPer; ++e) o[e] *= alpha;
-      // A key at a time for all of V's elements, eight of them in flight.
+      // A key at a time for all of V's elements, four of them in flight.
       auto add = [&](int j) {
         const float pj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), j));
         const char* vr = v0 + ((uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(v_at >> 32), j))) << 32) |
@@ -104,9 +104,9 @@ __device__ void attend_row(const PagedAttendArgs& a, int s, const QueryRow& qr, 
       };
       if (!dead) {
         int j = 0;
-        for (; j + 8 <= n; j += 8) {
+        for (; j + 4 <= n; j += 4) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) add(j + i);
+          for (int i = 0; i < 4; ++i) add(j + i);
         }
         for (; j < n; ++j) add(j);
         bool nan = true;
@@ -162,11 +162,7 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
   } else if (g > 0 && g < groups) {
     parts = join;
   }
-  // Blocks of 32 rows of whole tiles, none if no attention since the plan marked any: thread t of block b looks at
-  // number b, and t times as many as there are blocks behind it, so that marked ones lying together go to different blocks.
-  const int per_shift = shape.rows == 32 ? 0 : shape.rows == 128 ? 2 : 3;  // 32-row blocks of a tile
-  const int64_t jobs = h[14] ? (int64_t(tiles) * v.kv_heads) << per_shift : 0, blocks = int64_t(gridDim.x) * gridDim.y;
-  const int64_t job0 = int64_t(blockIdx.y) * gridDim.x + g;
+  const bool marks = h[14] != 0;
   Segment mine = {};
   bool again = false;
   if (parts > 1) {
@@ -281,35 +277,42 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
   }
 
   // Rows again: this block's, if joining them gave something that is not finite, and rows of whole tiles that the
-  // attention marked.  An infinity or NaN that every row sees marks them all, and key by key a row costs 130 times
-  // what it does by matrix (4680 rows of 12 heads over 23 400 keys: 86 ms), so they are spread over all blocks: 512
+  // attention marked.  An infinity or NaN that every row sees marks them all, and key by key a row costs 115 times
+  // what it does by matrix (4680 rows of 12 heads over 23 400 keys: 74 ms), so they are spread over all blocks: 512
   // tiles of 128 rows over 640 keys 1.7 ms, 895 with 256 tiles to a block.
-  for (int64_t j0 = job0; again || j0 < jobs; j0 += blocks * kFinishThreads) {
-    const int64_t at = j0 + tid * blocks;
-    const int mark =
-        at < jobs ? reinterpret_cast<const uint8_t*>(v.redo)[(at >> per_shift) * 8 + (at & ((1 << per_shift) - 1))] : 0;
-    if (!__syncthreads_or(mark) && !again) continue;
-    if (tid == 0) {
-      n_list = again;
-      list[0] = -1;
-    }
-    __syncthreads();
-    if (mark) list[atomicAdd(&n_list, 1)] = tid;
-    __syncthreads();
-    for (int i = 0; i < n_list; ++i) {
-      Segment s = mine;
-      int r0 = blockIdx.y * ROWS, r1 = min(r0 + ROWS, mine.rows);
-      if (list[i] >= 0) {
-        const int64_t job = j0 + list[i] * blocks;
-        s.task = int(job >> per_shift);
-        describe(v, shape, s);
-        r0 = 32 * int(job & ((1 << per_shift) - 1));
-        r1 = min(r0 + 32, s.rows);
+  if (again || marks) {
+    // Blocks of 32 rows of whole tiles, none if no attention since the plan marked any: thread t of block b looks at
+    // number b, and t times as many as there are blocks behind it, so that marked ones lying together go to different blocks.
+    const int per_shift = shape.rows == 32 ? 0 : shape.rows == 128 ? 2 : 3;  // 32-row blocks of a tile
+    const int64_t jobs = marks ? (int64_t(tiles) * v.kv_heads) << per_shift : 0, blocks = int64_t(gridDim.x) * gridDim.y;
+    const int64_t job0 = int64_t(blockIdx.y) * gridDim.x + g;
+    for (int64_t j0 = job0; again || j0 < jobs; j0 += blocks * kFinishThreads) {
+      const int64_t at = j0 + tid * blocks;
+      const int mark =
+          at < jobs ? reinterpret_cast<const uint8_t*>(v.redo)[(at >> per_shift) * 8 + (at & ((1 << per_shift) - 1))] : 0;
+      if (!__syncthreads_or(mark) && !again) continue;
+      if (tid == 0) {
+        n_list = again;
+        list[0] = -1;
       }
-      for (int r = r0 + wave; r < r1; r += kFinishWaves) attend_row<BF16, D>(a, s.seq, query_row(v, s, r), q_s[wave]);
+      __syncthreads();
+      if (mark) list[atomicAdd(&n_list, 1)] = tid;
+      __syncthreads();
+      for (int i = 0; i < n_list; ++i) {
+        Segment s = mine;
+        int r0 = blockIdx.y * ROWS, r1 = min(r0 + ROWS, mine.rows);
+        if (list[i] >= 0) {
+          const int64_t job = j0 + list[i] * blocks;
+          s.task = int(job >> per_shift);
+          describe(v, shape, s);
+          r0 = 32 * int(job & ((1 << per_shift) - 1));
+          r1 = min(r0 + 32, s.rows);
+        }
+        for (int r = r0 + wave; r < r1; r += kFinishWaves) attend_row<BF16, D>(a, s.seq, query_row(v, s, r), q_s[wave]);
+      }
+      again = false;
+      __syncthreads();
     }
-    again = false;
-    __syncthreads();
   }
   if (blockIdx.y > 0 || !refused) return;
 
