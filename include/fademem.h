@@ -513,7 +513,11 @@ int fademem_paged_insert(fademem_paged* paged, int32_t layer, const void* k, int
  * out_stride elements apart; out must not overlap q.  scale = 0 selects
  * 1/sqrt(D); negative scales are refused.  lse, if not NULL: [heads][rows]
  * fp32.  Keys that a row does not see do not reach it, whatever their values
- * (infinities and NaN too).
+ * (infinities and NaN too); rows whose result is not finite are worked out
+ * again key by key, which takes far longer than a call without them.
+ * FADEMEM_F32 holds 32 bits throughout.  FADEMEM_BF16: scores, row maxima, sums
+ * and O in fp32, the softmax weights rounded to bf16 for the products with V,
+ * weights below 2^-126 zero, O rounded once.
  * Errors: EINVAL, ESTATE (no step planned yet), EHIP. */
 int fademem_paged_attend(fademem_paged* paged, int32_t layer, const void* q, int64_t q_stride, float scale, void* out,
                          int64_t out_stride, float* lse, void* stream);

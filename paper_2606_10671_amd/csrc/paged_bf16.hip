@@ -10,6 +10,14 @@
 //
 // Rows are (token, head of the key head's group) pairs: a step of one token with
 // G heads per key head is one block of G rows.
+//
+// Scores, row maxima, sums and O are fp32.  Rounded to fewer bits are the weights P,
+// to bf16 (2^-8 of each at most): the matrix cores take P and V in one type, and
+// products of fp32 operands run at an eighth of the rate.  The row sum is that of
+// the weights before this rounding, whose errors average out over the keys: against
+// fp64 the output is off by its own rounding (24 ragged sequences: 1.70e-3 of the
+// output's root mean square, 1.65e-3 with weights in fp32).  The exponent
+// instruction makes a weight below 2^-126 zero, where the row's largest is 1 to 2^8.
 #include <type_traits>
 
 #include "paged_device.h"
@@ -315,9 +323,9 @@ __device__ __forceinline__ void paged_narrow_body(const PagedAttendArgs& a) {
 // unit's number; a tile that some row of the wave does not see whole is masked,
 // row by row; addresses come from the page table, read one tile before the loads
 // that need it.
-// 40 heads x 10 800 rows over 54 000 keys: 1.20 PFLOP/s, as near as 1% to a
-// product of two 8192 x 8192 matrices; 12 x 4680 rows over 23 400 keys 1.13, the matrix cores busy 61% of
-// the cycles.  Many short tasks are bound by what each costs beside its units, first
+// 40 heads x 10 800 rows over 54 000 keys: 1.09 to 1.20 PFLOP/s from one card to another, where a
+// product of two 8192 x 8192 matrices reaches 1.22; 12 x 4680 rows over 23 400 keys 1.05 to 1.13, the matrix cores
+// busy 61% of the cycles.  Many short tasks are bound by what each costs beside its units, first
 // loads and last results (24 ragged sequences, 16 heads of 64 over 4: 28 GFLOP in
 // 62 us).
 // ---------------------------------------------------------------------------

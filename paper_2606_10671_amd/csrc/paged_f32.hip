@@ -9,8 +9,10 @@
 // the rest of it enters in the one rounding that takes a score's distance to the
 // row max.  Bound by the matrix cores (2 x 64 MFMAs of 64 cycles per block at
 // D = 128) and by the softmax between them, which on a SIMD does not run beside fp32
-// MFMAs: 2 x 1170 rows of 12 heads over 5850 keys, 84 GFLOP in 775 us, matrix cores busy 74% of the
-// cycles.  Narrow tiles of few rows by those too, or by reading K and V.
+// MFMAs: 2 x 1170 rows of 12 heads over 5850 keys, 84 GFLOP in 769 to 836 us from one card to another, matrix cores
+// busy 73% of the cycles.  (1170 rows are nine tiles and 18 rows: the tenth costs as much as the others, for the work
+// of one wave of each split.)  Narrow tiles of few rows by those too, or by reading K and V.  The wide kernel at
+// D = 128 spills 16 registers around a segment's start and end, none inside the loop over its keys.
 #include "paged_device.h"
 
 namespace fademem {
@@ -40,7 +42,7 @@ struct Scale {
 // One tile of one wave: scores, weights, running max m and sum l (of this lane's
 // keys), O.  hide(key of the tile): true where the lane's row does not see it;
 // `hides`: some row of the wave does not see the whole tile.
-// `before_v` runs once the K tile is read, `after_scores` before V is.
+// `after_k` runs once the K tile is read, `before_v` before V is.
 template <int D, class Hide, class AfterK, class BeforeV>
 __device__ __forceinline__ void tile_f32(const f32x4 (&q)[D / 8], const float* kb, const float* vb, float rest, bool hides,
                                          Hide hide, AfterK after_k, BeforeV before_v, float& m, float& l,
