@@ -162,6 +162,7 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedAtten
   } else if (g > 0 && g < groups) {
     parts = join;
   }
+  static_assert(offsetof(PagedHeader, again) == offsetof(PagedHeader, groups) + 14 * sizeof(int32_t), "h[14]");
   const bool marks = h[14] != 0;
   Segment mine = {};
   bool again = false;

@@ -75,6 +75,8 @@ def check_spoiled(c, q, kv, lens, news, block, window, sinks, lse=True):
     at = 0
     for s, (have, n) in enumerate(zip(lens, news)):
         held = have + n
+        if n == 0:
+            continue
         k, v = (x.double().transpose(0, 1).repeat_interleave(heads // x.shape[1], 0).contiguous() for x in kv[s])
         p, j = torch.arange(have, held, device="cuda")[:, None] // block, torch.arange(held, device="cuda")[None] // block
         seen = j <= p
